@@ -54,7 +54,14 @@ typedef enum {
                               the buffers of its call (the access was skipped)           */
 } sbp_status;
 
-typedef enum { SBP_F32 = 0, SBP_BF16 = 1, SBP_I64 = 2 } sbp_dtype;
+typedef enum {
+  SBP_F32 = 0,
+  SBP_BF16 = 1,
+  SBP_I64 = 2,
+  SBP_E4M3 = 3 /* 8-bit floating point: 4 exponent bits, 3 mantissa bits, largest 448, no infinity.  Taken by
+                  sbp_local_shape and by the entry points on 8-bit blocks; every other one answers
+                  SBP_ERR_DTYPE.  (To box such a tensor, describe pairs of values as one BF16.) */
+} sbp_dtype;
 
 typedef enum {
   SBP_SPLIT = 0,
@@ -96,7 +103,8 @@ typedef struct {
  *                    replica (Table 2: B -> S costs nothing, see sbp_view_b_to_s) or a sub-block of a
  *                    matrix.  Honoured by sbp_matmul (all three tensors), by sbp_boxing on 2-D tensors
  *                    of one placement (S / B / P on either side, except the P(sum)-destination and
- *                    cast rows) and by sbp_softmax_xent / sbp_softmax_xent_backward (logits, grad);
+ *                    cast rows), by sbp_softmax_xent / sbp_softmax_xent_backward (logits, grad), and by layer
+ *                    norm and the entry points on 8-bit blocks for every tensor but scales and row or column vectors;
  *                    every other entry point answers SBP_ERR_UNSUPPORTED to a non-dense tensor.
  */
 typedef struct {
@@ -513,6 +521,76 @@ sbp_status sbp_embedding(const sbp_tensor* table, const sbp_tensor* ids, sbp_ten
  * should the second LAUNCH itself fail (SBP_ERR_CUDA) the gradient has already been zeroed. */
 sbp_status sbp_embedding_backward(const sbp_tensor* grad_out, const sbp_tensor* ids, sbp_tensor* grad_table,
                                   int32_t* oob_count, void* cuda_stream);
+
+/* ---------------------------------------------------------------- layer norm
+ *
+ * (No counterpart in the paper; like everything below it: what a transformer layer needs around the products of Table 1.)
+ * Rows of n elements, n the last extent, are normalised by their own mean and deviation:
+ *   mean = sum x / n     rstd = 1 / sqrt(sum (x - mean)^2 / n + eps)     y = (x - mean) rstd gamma + beta
+ *   x      [..., n]  F32 or BF16, 2 to 4 axes; S(i) of any axis but the last, or B
+ *   gamma  [n]       B, F32 or BF16; NULL: ones
+ *   beta   [n]       B, F32 or BF16; NULL: zeros
+ *   y      as x in shape, signature and placement; F32 or BF16
+ *   mean   [...]     x's shape without its last axis, x's signature, F32; NULL: not wanted (so rstd)
+ * Sums are held in fp32, the squares are those of differences from the mean.  A row that holds a NaN or an infinity
+ * is NaN; other rows are not affected.  n >= 1; no rows at all is fine.  eps >= 0 (a row of equal elements and eps 0: NaN).
+ * A B tensor's replicas are each normalised by themselves, buffers that are shared by all of them once. */
+sbp_status sbp_layer_norm(const sbp_tensor* x, const sbp_tensor* gamma, const sbp_tensor* beta, sbp_tensor* y, sbp_tensor* mean,
+                          sbp_tensor* rstd, float eps, void* cuda_stream);
+
+/* Its backward pass: with h = (x - mean) rstd and a = grad_y gamma,
+ *   grad_x     = rstd (a - sum a / n - h sum (a h) / n)
+ *   grad_gamma = sum over rows of grad_y h          grad_beta = sum over rows of grad_y
+ *   x, gamma, mean, rstd        as given to and written by the forward pass
+ *   grad_y  as y (F32 or BF16)  grad_x  as x, F32 or BF16
+ *   grad_gamma, grad_beta  [n]  F32, of one signature; either may be NULL.  x S(i): P(sum), every shard's sum over its own rows; or B
+ *                               (data parallelism's all-reduce folded in) or S(0) (its reduce-scatter).  x B: B or S(0).
+ * Sums over rows are made in a fixed order: the same call gives the same bits.  ws holds the blocks' sums (scratch; not
+ * looked at and may be NULL where both gradients are); 16-byte aligned; the size is asked of the device that is current. */
+size_t sbp_layer_norm_backward_workspace_bytes(const sbp_tensor* x);
+sbp_status sbp_layer_norm_backward(const sbp_tensor* x, const sbp_tensor* gamma, const sbp_tensor* mean, const sbp_tensor* rstd,
+                                   const sbp_tensor* grad_y, sbp_tensor* grad_x, sbp_tensor* grad_gamma, sbp_tensor* grad_beta, void* ws,
+                                   size_t ws_bytes, void* cuda_stream);
+
+/* ---------------------------------------------------------------- 8-bit blocks
+ *
+ * A tensor in 8 bits is two tensors: `values`, SBP_E4M3, and `scales`, SBP_F32, one number for each block of 128 elements along the
+ * last axis (the last block of a row may be shorter) or, for matrices, for each tile of 128 x 128; an element stands for
+ * value * scale.  Blocks are those of the LOCAL tensors, each counted from its own start.  scales has the signature and placement
+ * of values; its last extent (for tiles: both) is the sum over the shards of ceil(local extent / 128) along an axis that is split,
+ * else ceil(extent / 128) -- sbp_scales_shape tells it -- and its balanced split then gives every shard
+ * the scales of its own blocks.
+ * quantize8 takes scales that are powers of two: 2^e with the smallest e >= -126 for which no finite element of the block
+ * exceeds 448 * 2^e in magnitude (1 for a block of zeros), so an element is rounded once, to nearest even.  Infinities and NaN become NaN and
+ * leave their block's scale alone.  Products and gradients take any fp32 scale. */
+#define SBP_QUANT_TILES 8u
+sbp_status sbp_scales_shape(const sbp_tensor* values, uint32_t flags /* 0 or SBP_QUANT_TILES */, int64_t out_shape[SBP_MAX_DIMS]);
+
+/* x (F32 or BF16) into 8-bit blocks.  flags: SBP_QUANT_TILES: a scale a tile (2-D only).  SBP_TRANS_X (2-D only): values is the
+ * transpose of x, blocks along x's rows; a stored S(0) of x is S(1) of values and the other way round: an operand whose contraction
+ * runs along its rows becomes one whose contraction is its last axis.  Signatures: S(i) or B (P: quantising is not linear). */
+sbp_status sbp_quantize8(const sbp_tensor* x, sbp_tensor* values, sbp_tensor* scales, uint32_t flags, void* cuda_stream);
+
+/* GeLU that keeps its input for the backward pass in 8 bits: y = z/2 (1 + erf(z / sqrt 2)), computed in fp32 (relative error below 2^-20),
+ * F32 or BF16 like z, in one pass with values / scales = the blocks of z as sbp_quantize8(z) makes them.  All of one
+ * shape and signature, S(i) or B. */
+sbp_status sbp_gelu_save8(const sbp_tensor* z, sbp_tensor* y, sbp_tensor* values, sbp_tensor* scales, void* cuda_stream);
+
+/* Gradient through it: grad_z = grad_y (Phi(z) + z phi(z)), Phi and phi the normal distribution and density, z = value * scale.
+ * grad_y and grad_z F32 or BF16.  Scales of 1 x 128 blocks. */
+sbp_status sbp_gelu_save8_backward(const sbp_tensor* values, const sbp_tensor* scales, const sbp_tensor* grad_y, sbp_tensor* grad_z,
+                                   void* cuda_stream);
+
+/* MatMul of two 8-bit operands: Y = X W, X given as values [M,K], W as its transpose, values [N,K] (as with SBP_TRANS_W of sbp_matmul: a stored S(0)
+ * counts as S(1) and the other way round), so that both operands' blocks run along the contraction:
+ *   y[m,n] = sum over blocks b of  x_scales[m,b] w_scales[n,b]  sum over k in b of  x[m,k] w[n,k]
+ * with a row per element or per 128 (tiles) in either scales tensor, told apart by their first extent.  Signatures, fused results and
+ * replicas as sbp_matmul (one-axis placements); y F32 or BF16.
+ * A block's products are summed in fp32 on the tensor cores and its sum, scaled, is added to fp32 registers; few rows or columns are
+ * cut along K over the CTAs of a cluster and joined in a fixed order.  Values whose base or leading dimension is not a multiple of 16
+ * bytes are multiplied by a slower form of the kernel.  No workspace. */
+sbp_status sbp_matmul8(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales, sbp_tensor* y,
+                       void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -24,6 +24,7 @@ from __future__ import annotations
 
 import numpy as np
 from scipy.special import erf as _erf
+from scipy.special import erfc as _erfc
 
 S0 = ("S", 0)
 S1 = ("S", 1)
@@ -478,3 +479,82 @@ def embedding_grad_table(grad_out, ids, rows):
     np.add.at(out, ids[ok], g[ok])
     return out
 
+
+
+# ------------------------------------------------------------------ layer norm
+
+def layer_norm(x, gamma, beta, eps):
+    """(y, mean, rstd) over the last axis, fp64."""
+    x = np.asarray(x, dtype=np.float64)
+    mean = x.mean(-1)
+    rstd = 1.0 / np.sqrt(((x - mean[..., None]) ** 2).mean(-1) + eps)
+    h = (x - mean[..., None]) * rstd[..., None]
+    return h * gamma + beta, mean, rstd
+
+
+def layer_norm_grads(x, gamma, mean, rstd, grad_y):
+    """(grad_x, grad_gamma, grad_beta) for given mean and rstd, fp64; x and grad_y as matrices."""
+    x, dy = np.asarray(x, dtype=np.float64), np.asarray(grad_y, dtype=np.float64)
+    mean, rstd = np.asarray(mean, dtype=np.float64)[:, None], np.asarray(rstd, dtype=np.float64)[:, None]
+    h, a = (x - mean) * rstd, dy * gamma
+    n = x.shape[1]
+    dx = rstd * (a - a.sum(1, keepdims=True) / n - h * (a * h).sum(1, keepdims=True) / n)
+    return dx, (dy * h).sum(0), dy.sum(0)
+
+
+# ------------------------------------------------------------------ 8-bit blocks
+
+BLOCK8 = 128
+
+
+def round_to_e4m3(v):
+    """Nearest e4m3 number (ties to even) of finite numbers of magnitude up to 448, NaN for what is not finite; fp64."""
+    v = np.asarray(v, dtype=np.float64)
+    fine = np.isfinite(v)
+    w = np.where(fine, v, 0.0)
+    _, ex = np.frexp(w)                                 # |w| = m 2^ex, m in [0.5, 1)
+    step = np.ldexp(1.0, np.maximum(ex - 1, -6) - 3)
+    return np.where(fine, np.rint(w / step) * step, np.nan)
+
+
+def quantize8(x, tiles=False):
+    """(values, scales) of a matrix in fp64: per 128 along a row, or per 128 x 128, the smallest power of two 2^e, e >= -126,
+    under which no finite element exceeds 448 (1 for a block of zeros)."""
+    x = np.asarray(x, dtype=np.float64)
+    rows, cols = x.shape
+    height = BLOCK8 if tiles else 1
+    nr, nc = -(-rows // height), -(-cols // BLOCK8)
+    scales = np.ones((nr, nc))
+    q = np.empty_like(x)
+    for i in range(nr):
+        for j in range(nc):
+            at = (slice(i * height, (i + 1) * height), slice(j * BLOCK8, (j + 1) * BLOCK8))
+            b = x[at]
+            mag = np.abs(b[np.isfinite(b)])
+            big = mag.max() if mag.size else 0.0
+            if big > 0:
+                e = -126
+                while big > 448.0 * 2.0 ** e:
+                    e += 1
+                scales[i, j] = 2.0 ** e
+            q[at] = round_to_e4m3(b / scales[i, j])
+    return q, scales
+
+
+def dequantize8(values, scales, tiles=False):
+    rows, cols = np.shape(values)
+    s = np.repeat(np.asarray(scales, dtype=np.float64), BLOCK8, 1)[:, :cols]
+    if tiles:
+        s = np.repeat(s, BLOCK8, 0)[:rows]
+    return np.asarray(values, dtype=np.float64) * s
+
+
+def gelu_from_erfc(z):
+    """GeLU by the complementary error function, exact in the lower tail too, fp64."""
+    z = np.asarray(z, dtype=np.float64)
+    return 0.5 * z * _erfc(-z / np.sqrt(2.0))
+
+
+def gelu_slope(z):
+    z = np.asarray(z, dtype=np.float64)
+    return 0.5 * _erfc(-z / np.sqrt(2.0)) + z * np.exp(-0.5 * z * z) / np.sqrt(2.0 * np.pi)

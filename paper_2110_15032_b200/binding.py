@@ -15,9 +15,10 @@ SBP_MAX_PDIMS = 2
 SBP_EPILOGUE_GELU = 1
 SBP_TRANS_X = 2
 SBP_TRANS_W = 4
+SBP_QUANT_TILES = 8
 
 SBP_SPLIT, SBP_BROADCAST, SBP_PARTIAL_SUM, SBP_PARTIAL_MAX = 0, 1, 2, 3
-_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.int64: 2}
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.int64: 2, torch.float8_e4m3fn: 3}
 
 
 class _Sig(C.Structure):
@@ -144,6 +145,15 @@ def load_library():
     lib.sbp_softmax_xent_static.argtypes = [T, T, T, T, T, C.c_void_p]
     lib.sbp_embedding.argtypes = [T, T, T, C.c_void_p, C.c_void_p]
     lib.sbp_embedding_backward.argtypes = [T, T, T, C.c_void_p, C.c_void_p]
+    lib.sbp_layer_norm.argtypes = [T, T, T, T, T, T, C.c_float, C.c_void_p]
+    lib.sbp_layer_norm_backward_workspace_bytes.restype = C.c_size_t
+    lib.sbp_layer_norm_backward_workspace_bytes.argtypes = [T]
+    lib.sbp_layer_norm_backward.argtypes = [T, T, T, T, T, T, T, T, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.sbp_scales_shape.argtypes = [T, C.c_uint32, C.POINTER(C.c_int64)]
+    lib.sbp_quantize8.argtypes = [T, T, T, C.c_uint32, C.c_void_p]
+    lib.sbp_gelu_save8.argtypes = [T, T, T, T, C.c_void_p]
+    lib.sbp_gelu_save8_backward.argtypes = [T, T, T, T, C.c_void_p]
+    lib.sbp_matmul8.argtypes = [T, T, T, T, T, C.c_void_p]
     _LIB = lib
     return lib
 
@@ -151,7 +161,8 @@ def load_library():
 # Entry points called through the native module, in the order its bind() takes them.
 _NATIVE_ENTRIES = ("sbp_boxing", "sbp_boxing_shard", "sbp_matmul", "sbp_softmax_xent", "sbp_softmax_xent_static",
                    "sbp_softmax_xent_backward", "sbp_matmul_softmax_xent", "sbp_matmul_softmax_xent_backward",
-                   "sbp_embedding", "sbp_embedding_backward")
+                   "sbp_embedding", "sbp_embedding_backward", "sbp_layer_norm", "sbp_layer_norm_backward", "sbp_quantize8",
+                   "sbp_gelu_save8", "sbp_gelu_save8_backward", "sbp_matmul8")
 _NATIVE = None
 
 
@@ -533,5 +544,70 @@ def sbp_embedding(table: SbpTensor, ids: SbpTensor, out: SbpTensor,
 def sbp_embedding_backward(grad_out: SbpTensor, ids: SbpTensor, grad_table: SbpTensor,
                            oob_count: Optional[torch.Tensor] = None, stream=None) -> None:
     st = (_NATIVE or _native()).embedding_backward(grad_out, ids, grad_table, oob_count, stream)
+    if st:
+        _check(st)
+
+
+def sbp_layer_norm(x: SbpTensor, gamma: Optional[SbpTensor], beta: Optional[SbpTensor], y: SbpTensor,
+                   mean: Optional[SbpTensor] = None, rstd: Optional[SbpTensor] = None, eps: float = 1e-5, stream=None) -> None:
+    """y = (x - mean) rstd gamma + beta over the last axis; mean and rstd are kept for the backward pass where they are given."""
+    st = (_NATIVE or _native()).layer_norm(x, gamma, beta, y, mean, rstd, eps, stream)
+    if st:
+        _check(st)
+
+
+def sbp_layer_norm_backward_workspace_bytes(x: SbpTensor) -> int:
+    a = x._c()
+    return int(load_library().sbp_layer_norm_backward_workspace_bytes(C.byref(a)))
+
+
+def sbp_layer_norm_backward(x: SbpTensor, gamma: Optional[SbpTensor], mean: SbpTensor, rstd: SbpTensor, grad_y: SbpTensor,
+                            grad_x: SbpTensor, grad_gamma: Optional[SbpTensor] = None, grad_beta: Optional[SbpTensor] = None,
+                            ws: Optional[torch.Tensor] = None, stream=None) -> None:
+    """grad_x, and summed over the rows grad_gamma and grad_beta as P(sum), B or S(0)."""
+    st = (_NATIVE or _native()).layer_norm_backward(x, gamma, mean, rstd, grad_y, grad_x, grad_gamma, grad_beta, ws, stream)
+    if st:
+        _check(st)
+
+
+def sbp_scales_shape(values_shape, sig: Sig, k: int, flags: int = 0):
+    """Global shape of the scales of an 8-bit tensor of this shape, signature and placement (flags: 0 or SBP_QUANT_TILES)."""
+    d = _Tensor()
+    d.ndim = len(values_shape)
+    d.dtype = _DTYPES[torch.float8_e4m3fn]
+    for i, s in enumerate(values_shape):
+        d.shape[i] = int(s)
+    d.pdims = 1
+    d.pshape[0], d.pshape[1] = int(k), 1
+    d.sbp[0] = sig._c()
+    out = (C.c_int64 * SBP_MAX_DIMS)()
+    _check(load_library().sbp_scales_shape(C.byref(d), flags, out))
+    return tuple(out[i] for i in range(len(values_shape)))
+
+
+def sbp_quantize8(x: SbpTensor, values: SbpTensor, scales: SbpTensor, flags: int = 0, stream=None) -> None:
+    """x as 8-bit blocks: e4m3 values (torch.float8_e4m3fn) and fp32 scales; flags SBP_QUANT_TILES, SBP_TRANS_X."""
+    st = (_NATIVE or _native()).quantize8(x, values, scales, flags, stream)
+    if st:
+        _check(st)
+
+
+def sbp_gelu_save8(z: SbpTensor, y: SbpTensor, values: SbpTensor, scales: SbpTensor, stream=None) -> None:
+    """y = GeLU(z), and z in 8-bit blocks for the backward pass."""
+    st = (_NATIVE or _native()).gelu_save8(z, y, values, scales, stream)
+    if st:
+        _check(st)
+
+
+def sbp_gelu_save8_backward(values: SbpTensor, scales: SbpTensor, grad_y: SbpTensor, grad_z: SbpTensor, stream=None) -> None:
+    """grad_z = grad_y times GeLU's slope at the z that values and scales hold."""
+    st = (_NATIVE or _native()).gelu_save8_backward(values, scales, grad_y, grad_z, stream)
+    if st:
+        _check(st)
+
+
+def sbp_matmul8(x: SbpTensor, x_scales: SbpTensor, w: SbpTensor, w_scales: SbpTensor, y: SbpTensor, stream=None) -> None:
+    """Y = X W of 8-bit operands, W given as its transpose [N, K] (see include/sbp.h)."""
+    st = (_NATIVE or _native()).matmul8(x, x_scales, w, w_scales, y, stream)
     if st:
         _check(st)

@@ -76,6 +76,7 @@ bool fill(PyObject* obj, sbp_tensor* d) {
     case at::kFloat: d->dtype = SBP_F32; break;
     case at::kBFloat16: d->dtype = SBP_BF16; break;
     case at::kLong: d->dtype = SBP_I64; break;
+    case at::kFloat8_e4m3fn: d->dtype = SBP_E4M3; break;
     default: PyErr_SetObject(PyExc_KeyError, dtype.p); return false;
   }
   d->pdims = (int32_t)np;
@@ -147,13 +148,19 @@ struct {
   sbp_status (*matmul_softmax_xent_backward)(const T*, const T*, const T*, const T*, const T*, T*, void*);
   sbp_status (*embedding)(const T*, const T*, T*, int32_t*, void*);
   sbp_status (*embedding_backward)(const T*, const T*, T*, int32_t*, void*);
+  sbp_status (*layer_norm)(const T*, const T*, const T*, T*, T*, T*, float, void*);
+  sbp_status (*layer_norm_backward)(const T*, const T*, const T*, const T*, const T*, T*, T*, T*, void*, size_t, void*);
+  sbp_status (*quantize8)(const T*, T*, T*, uint32_t, void*);
+  sbp_status (*gelu_save8)(const T*, T*, T*, T*, void*);
+  sbp_status (*gelu_save8_backward)(const T*, const T*, const T*, T*, void*);
+  sbp_status (*matmul8)(const T*, const T*, const T*, const T*, T*, void*);
 } lib;
 
 // Arguments: the first n_desc are SbpTensors (those of the bits in `optional` may be None), the last is the
 // stream or None; what lies between is the caller's.
 struct Call {
-  T d[6];
-  T* at[6];
+  T d[8];
+  T* at[8];
   void* stream;
   bool ok;
   Call(const char* name, PyObject* const* args, Py_ssize_t n, Py_ssize_t want, int n_desc, unsigned optional) : ok(false) {
@@ -240,6 +247,33 @@ ENTRY(embedding_backward) {
           RUN(lib.embedding_backward(c.at[0], c.at[1], c.at[2], static_cast<int32_t*>(oob), c.stream));)
 }
 
+ENTRY(layer_norm) {
+  GUARDED(Call c("layer_norm", args, n, 8, 6, 0x36); if (!c.ok) return nullptr; const double eps = PyFloat_AsDouble(args[6]);
+          if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+          RUN(lib.layer_norm(c.at[0], c.at[1], c.at[2], c.at[3], c.at[4], c.at[5], (float)eps, c.stream));)
+}
+ENTRY(layer_norm_backward) {
+  GUARDED(Call c("layer_norm_backward", args, n, 10, 8, 0xc2); void* ws; size_t bytes;
+          if (!c.ok || !memory_of(args[8], true, &ws, &bytes)) return nullptr;
+          RUN(lib.layer_norm_backward(c.at[0], c.at[1], c.at[2], c.at[3], c.at[4], c.at[5], c.at[6], c.at[7], ws, bytes, c.stream));)
+}
+ENTRY(quantize8) {
+  GUARDED(Call c("quantize8", args, n, 5, 3, 0); int64_t flags; if (!c.ok || !as_i64(args[3], &flags)) return nullptr;
+          RUN(lib.quantize8(c.at[0], c.at[1], c.at[2], (uint32_t)flags, c.stream));)
+}
+ENTRY(gelu_save8) {
+  GUARDED(Call c("gelu_save8", args, n, 5, 4, 0); if (!c.ok) return nullptr;
+          RUN(lib.gelu_save8(c.at[0], c.at[1], c.at[2], c.at[3], c.stream));)
+}
+ENTRY(gelu_save8_backward) {
+  GUARDED(Call c("gelu_save8_backward", args, n, 5, 4, 0); if (!c.ok) return nullptr;
+          RUN(lib.gelu_save8_backward(c.at[0], c.at[1], c.at[2], c.at[3], c.stream));)
+}
+ENTRY(matmul8) {
+  GUARDED(Call c("matmul8", args, n, 6, 5, 0); if (!c.ok) return nullptr;
+          RUN(lib.matmul8(c.at[0], c.at[1], c.at[2], c.at[3], c.at[4], c.stream));)
+}
+
 // bind(addresses): the library's entry points, in the order of `lib`, from the library the process loaded.
 PyObject* py_bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   constexpr Py_ssize_t kEntries = sizeof(lib) / sizeof(void*);
@@ -271,6 +305,12 @@ PyMethodDef methods[] = {METHOD(bind),
                          METHOD(matmul_softmax_xent_backward),
                          METHOD(embedding),
                          METHOD(embedding_backward),
+                         METHOD(layer_norm),
+                         METHOD(layer_norm_backward),
+                         METHOD(quantize8),
+                         METHOD(gelu_save8),
+                         METHOD(gelu_save8_backward),
+                         METHOD(matmul8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

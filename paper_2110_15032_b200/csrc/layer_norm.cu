@@ -1,0 +1,729 @@
+// Layer norm over the last axis, forward and backward, with the reduction of gamma's and beta's gradients over the rows.
+//
+// Bound: DRAM.  Forward a row is read once, kept in registers for mean, squares and result, and written once; backward the same of x and
+// grad_y, while every thread adds up grad_y h and grad_y of its columns over the rows that its block takes.  A block's sums go to the
+// workspace, and a second kernel adds the blocks' up, always in the same order: P(sum), the all-reduce and the reduce-scatter of data
+// parallelism are which blocks it adds and where it stores.
+//
+// G threads share a row, each with NV times eight of its elements.  Rows too long for registers (over 16384) are read again for
+// each pass, out of L2.
+#include "blocks8.h"
+
+namespace sbp {
+
+namespace {
+
+struct NormJob {
+  const void* x;
+  const void* dy;      // backward
+  void* out;           // y, or grad_x
+  float* mean;
+  float* rstd;
+  long long rows, ldx, lddy, ldo;
+};
+struct NormParams {
+  NormJob j[SBP_MAX_K];
+  const void* gamma;   // null: ones
+  const void* beta;    // null: zeros
+  int gamma_f32, beta_f32;
+  long long cols;
+  float eps;
+  float* parts;        // backward: [job * blocks of a job + block][2][cols]; null: the sums are not wanted
+  int first_only;      // the jobs are replicas: the sums of the first one's rows are wanted
+};
+
+__device__ __forceinline__ float vector_at(const void* p, int f32, long long c, float none) {
+  if (!p) return none;
+  if (f32) return SBP_GUARD(static_cast<const float*>(p) + c, 4) ? static_cast<const float*>(p)[c] : 0.f;
+  return SBP_GUARD(static_cast<const __nv_bfloat16*>(p) + c, 2) ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[c]) : 0.f;
+}
+
+// Where thread t of G finds its elements of chunk i (8 G elements): VEC eight that follow one another, else every G-th.
+template <int G, bool VEC>
+struct Piece {
+  long long col;
+  int n;
+  static constexpr int step = VEC ? 1 : G;
+  __device__ __forceinline__ Piece(int i, int t, long long cols) {
+    col = (long long)i * (8 * G) + (VEC ? t * 8 : t);
+    if constexpr (VEC) n = col < cols ? 8 : 0;
+    else n = col < cols ? (int)min((cols - col + G - 1) / G, 8LL) : 0;
+  }
+};
+
+// Sums over the G threads of a row; G over 32 is the whole block.  `turn` alternates between two buffers, so one barrier does.
+template <int G, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float (*buf)[N][32], int& turn) {
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s[k] += __shfl_xor_sync(0xffffffffu, s[k], d);
+  if constexpr (G > 32) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) buf[turn][k][warp] = s[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      float v = lane < G / 32 ? buf[turn][k][lane] : 0.f;
+#pragma unroll
+      for (int d = G / 64; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+      s[k] = __shfl_sync(0xffffffffu, v, 0);
+    }
+    turn ^= 1;
+  }
+}
+
+constexpr int norm_threads(int g) { return g > 32 ? g : 256; }
+
+template <typename TX, typename TY, int G, int NV, bool VEC>
+__global__ void __launch_bounds__(norm_threads(G)) norm_kernel(const __grid_constant__ NormParams P) {
+  constexpr int kGroups = norm_threads(G) / G;
+  __shared__ float red[2][1][32];
+  SBP_PDL_RELEASE();
+  SBP_PDL_WAIT();
+  const NormJob& J = P.j[blockIdx.y];
+  const int t = threadIdx.x % G;
+  const float inv_n = 1.0f / (float)P.cols;
+  float ga[NV][8], be[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const Piece<G, VEC> at(i, t, P.cols);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      ga[i][e] = e < at.n ? vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f) : 0.f;
+      be[i][e] = e < at.n ? vector_at(P.beta, P.beta_f32, at.col + e * at.step, 0.f) : 0.f;
+    }
+  }
+  int turn = 0;
+  for (long long row = (long long)blockIdx.x * kGroups + threadIdx.x / G; row < J.rows; row += (long long)gridDim.x * kGroups) {
+    float v[NV][8];
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Piece<G, VEC> at(i, t, P.cols);
+      if (at.n > 0) load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, v[i], at.n, at.step);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < at.n) s[0] += v[i][e];
+    }
+    row_sums<G>(s, red, turn);
+    const float mean = s[0] * inv_n;
+    s[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Piece<G, VEC> at(i, t, P.cols);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[i][e] -= mean;
+        if (e < at.n) s[0] = fmaf(v[i][e], v[i][e], s[0]);
+      }
+    }
+    row_sums<G>(s, red, turn);
+    const float rstd = 1.0f / sqrtf(fmaf(s[0], inv_n, P.eps));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Piece<G, VEC> at(i, t, P.cols);
+      if (at.n > 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * rstd, ga[i][e], be[i][e]);
+        store8<VEC>(static_cast<TY*>(J.out) + row * J.ldo + at.col, v[i], at.n, at.step);
+      }
+    }
+    if (t == 0) {
+      if (J.mean && SBP_GUARD(J.mean + row, 4)) J.mean[row] = mean;
+      if (J.rstd && SBP_GUARD(J.rstd + row, 4)) J.rstd[row] = rstd;
+    }
+  }
+}
+
+template <typename TX, typename TY, int G, int NV, bool VEC>
+__global__ void __launch_bounds__(norm_threads(G)) norm_grad_kernel(const __grid_constant__ NormParams P) {
+  constexpr int kGroups = norm_threads(G) / G;
+  __shared__ float red[2][2][32];
+  SBP_PDL_RELEASE();
+  SBP_PDL_WAIT();
+  const NormJob& J = P.j[blockIdx.y];
+  const int t = threadIdx.x % G;
+  const float inv_n = 1.0f / (float)P.cols;
+  float ga[NV][8], sum_g[NV][8], sum_b[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const Piece<G, VEC> at(i, t, P.cols);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      ga[i][e] = e < at.n ? vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f) : 0.f;
+      sum_g[i][e] = sum_b[i][e] = 0.f;
+    }
+  }
+  int turn = 0;
+  for (long long row = (long long)blockIdx.x * kGroups + threadIdx.x / G; row < J.rows; row += (long long)gridDim.x * kGroups) {
+    float h[NV][8], d[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Piece<G, VEC> at(i, t, P.cols);
+      if (at.n > 0) {
+        load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, h[i], at.n, at.step);
+        load8<VEC>(static_cast<const TY*>(J.dy) + row * J.lddy + at.col, d[i], at.n, at.step);
+      }
+    }
+    const float mean = SBP_GUARD(J.mean + row, 4) ? J.mean[row] : 0.f, rstd = SBP_GUARD(J.rstd + row, 4) ? J.rstd[row] : 0.f;
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Piece<G, VEC> at(i, t, P.cols);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < at.n) {
+          h[i][e] = (h[i][e] - mean) * rstd;
+          sum_g[i][e] = fmaf(d[i][e], h[i][e], sum_g[i][e]);
+          sum_b[i][e] += d[i][e];
+          d[i][e] *= ga[i][e];
+          s[0] += d[i][e];
+          s[1] = fmaf(d[i][e], h[i][e], s[1]);
+        }
+    }
+    row_sums<G>(s, red, turn);
+    const float a = s[0] * inv_n, b = s[1] * inv_n;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Piece<G, VEC> at(i, t, P.cols);
+      if (at.n > 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[i][e] = rstd * (d[i][e] - a - h[i][e] * b);
+        store8<VEC>(static_cast<TX*>(J.out) + row * J.ldo + at.col, d[i], at.n, at.step);
+      }
+    }
+  }
+  if (!P.parts || (P.first_only && blockIdx.y > 0)) return;
+  float* part = P.parts + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 2 * P.cols;
+  if constexpr (kGroups > 1) {      // the block's rows together, group by group
+    __shared__ float joined[kGroups][8 * G * NV];
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const Piece<G, VEC> at(i, t, P.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < at.n) joined[threadIdx.x / G][at.col + e * at.step] = which ? sum_b[i][e] : sum_g[i][e];
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < P.cols; c += norm_threads(G)) {
+        float v = joined[0][c];
+#pragma unroll
+        for (int w = 1; w < kGroups; ++w) v += joined[w][c];
+        float* to = part + which * P.cols + c;
+        if (SBP_GUARD(to, 4)) *to = v;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Piece<G, VEC> at(i, t, P.cols);
+      if (at.n > 0) {
+        store8<VEC>(part + at.col, sum_g[i], at.n, at.step);
+        store8<VEC>(part + P.cols + at.col, sum_b[i], at.n, at.step);
+      }
+    }
+  }
+}
+
+// Rows longer than registers hold: a block a row, read once a pass.
+constexpr int kWide = 512;
+template <typename TX, typename TY, bool VEC>
+__global__ void __launch_bounds__(kWide) norm_wide_kernel(const __grid_constant__ NormParams P) {
+  __shared__ float red[2][1][32];
+  SBP_PDL_RELEASE();
+  SBP_PDL_WAIT();
+  const NormJob& J = P.j[blockIdx.y];
+  const int t = threadIdx.x, chunks = (int)((P.cols + 8 * kWide - 1) / (8 * kWide));
+  const float inv_n = 1.0f / (float)P.cols;
+  int turn = 0;
+  for (long long row = blockIdx.x; row < J.rows; row += gridDim.x) {
+    const TX* x = static_cast<const TX*>(J.x) + row * J.ldx;
+    float mean = 0.f, s[1], v[8];
+    for (int pass = 0; pass < 2; ++pass) {      // the sum, then the squares of what differs from the mean
+      s[0] = 0.f;
+      for (int i = 0; i < chunks; ++i) {
+        const Piece<kWide, VEC> at(i, t, P.cols);
+        if (at.n == 0) continue;
+        load8<VEC>(x + at.col, v, at.n, at.step);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < at.n) s[0] += pass ? (v[e] - mean) * (v[e] - mean) : v[e];
+      }
+      row_sums<kWide>(s, red, turn);
+      if (pass == 0) mean = s[0] * inv_n;
+    }
+    const float rstd = 1.0f / sqrtf(fmaf(s[0], inv_n, P.eps));
+    for (int i = 0; i < chunks; ++i) {
+      const Piece<kWide, VEC> at(i, t, P.cols);
+      if (at.n == 0) continue;
+      load8<VEC>(x + at.col, v, at.n, at.step);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < at.n)
+          v[e] = fmaf((v[e] - mean) * rstd, vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f),
+                      vector_at(P.beta, P.beta_f32, at.col + e * at.step, 0.f));
+      store8<VEC>(static_cast<TY*>(J.out) + row * J.ldo + at.col, v, at.n, at.step);
+    }
+    if (t == 0) {
+      if (J.mean && SBP_GUARD(J.mean + row, 4)) J.mean[row] = mean;
+      if (J.rstd && SBP_GUARD(J.rstd + row, 4)) J.rstd[row] = rstd;
+    }
+  }
+}
+
+template <typename TX, typename TY, bool VEC>
+__global__ void __launch_bounds__(kWide) norm_grad_wide_kernel(const __grid_constant__ NormParams P) {
+  __shared__ float red[2][2][32];
+  SBP_PDL_RELEASE();
+  SBP_PDL_WAIT();
+  const NormJob& J = P.j[blockIdx.y];
+  const int t = threadIdx.x, chunks = (int)((P.cols + 8 * kWide - 1) / (8 * kWide));
+  const float inv_n = 1.0f / (float)P.cols;
+  int turn = 0;
+  for (long long row = blockIdx.x; row < J.rows; row += gridDim.x) {
+    const TX* x = static_cast<const TX*>(J.x) + row * J.ldx;
+    const TY* dy = static_cast<const TY*>(J.dy) + row * J.lddy;
+    const float mean = SBP_GUARD(J.mean + row, 4) ? J.mean[row] : 0.f, rstd = SBP_GUARD(J.rstd + row, 4) ? J.rstd[row] : 0.f;
+    float s[2] = {0.f, 0.f}, h[8], d[8];
+    for (int i = 0; i < chunks; ++i) {
+      const Piece<kWide, VEC> at(i, t, P.cols);
+      if (at.n == 0) continue;
+      load8<VEC>(x + at.col, h, at.n, at.step);
+      load8<VEC>(dy + at.col, d, at.n, at.step);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < at.n) {
+          const float a = d[e] * vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f);
+          s[0] += a;
+          s[1] = fmaf(a, (h[e] - mean) * rstd, s[1]);
+        }
+    }
+    row_sums<kWide>(s, red, turn);
+    const float a = s[0] * inv_n, b = s[1] * inv_n;
+    for (int i = 0; i < chunks; ++i) {
+      const Piece<kWide, VEC> at(i, t, P.cols);
+      if (at.n == 0) continue;
+      load8<VEC>(x + at.col, h, at.n, at.step);
+      load8<VEC>(dy + at.col, d, at.n, at.step);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < at.n)
+          d[e] = rstd * (d[e] * vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f) - a - (h[e] - mean) * rstd * b);
+      store8<VEC>(static_cast<TX*>(J.out) + row * J.ldo + at.col, d, at.n, at.step);
+    }
+  }
+}
+
+// Their sums over the rows: a block takes 2048 columns and every gridDim.y-th row.
+constexpr int kWideCols = 256;
+template <typename TX, typename TY, bool VEC>
+__global__ void __launch_bounds__(kWideCols) norm_sums_wide_kernel(const __grid_constant__ NormParams P) {
+  SBP_PDL_RELEASE();
+  SBP_PDL_WAIT();
+  const NormJob& J = P.j[blockIdx.z];
+  const Piece<kWideCols, VEC> at((int)blockIdx.x, threadIdx.x, P.cols);
+  if (at.n == 0) return;
+  float sum_g[8] = {}, sum_b[8] = {};
+  for (long long row = blockIdx.y; row < J.rows; row += gridDim.y) {
+    float h[8], d[8];
+    load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, h, at.n, at.step);
+    load8<VEC>(static_cast<const TY*>(J.dy) + row * J.lddy + at.col, d, at.n, at.step);
+    const float mean = SBP_GUARD(J.mean + row, 4) ? J.mean[row] : 0.f, rstd = SBP_GUARD(J.rstd + row, 4) ? J.rstd[row] : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < at.n) {
+        sum_g[e] = fmaf(d[e], (h[e] - mean) * rstd, sum_g[e]);
+        sum_b[e] += d[e];
+      }
+  }
+  float* part = P.parts + ((long long)blockIdx.z * gridDim.y + blockIdx.y) * 2 * P.cols;
+  store8<VEC>(part + at.col, sum_g, at.n, at.step);
+  store8<VEC>(part + P.cols + at.col, sum_b, at.n, at.step);
+}
+
+// The blocks' sums added up: 32 columns a block, its eight warps each every eighth part of an output, then the warps in order.
+struct JoinParams {
+  const float* parts;
+  long long cols;
+  int per_job;                   // parts of a job
+  int lo[SBP_MAX_K], hi[SBP_MAX_K];      // jobs that output z is the sum of
+  float* out[2][SBP_MAX_K];      // [gamma, beta]; a gradient that is not wanted has nulls
+  int replicas;                  // > 0: output 0 goes to so many buffers
+  int split;                     // > 0: output 0 is split over so many shards
+};
+__global__ void __launch_bounds__(256) norm_join_kernel(const __grid_constant__ JoinParams P) {
+  __shared__ float sums[8][32];
+  SBP_PDL_RELEASE();
+  SBP_PDL_WAIT();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = blockIdx.y, z = blockIdx.z;
+  const long long c = (long long)blockIdx.x * 32 + lane;
+  if (!P.out[which][z]) return;
+  float v = 0.f;
+  if (c < P.cols) {
+    const int hi = P.hi[z] * P.per_job;
+    const float* from = P.parts + which * P.cols + c;
+#pragma unroll 8
+    for (int i = P.lo[z] * P.per_job + warp; i < hi; i += 8)
+      if (SBP_GUARD(from + i * 2 * P.cols, 4)) v += from[i * 2 * P.cols];
+  }
+  sums[warp][lane] = v;
+  __syncthreads();
+  if (warp == 0 && c < P.cols) {
+    v = sums[0][lane];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) v += sums[w][lane];
+    if (P.split > 0) {
+      int64_t start = 0, len = 0;
+      int r = 0;
+      for (; r < P.split; ++r) {
+        split_range(P.cols, P.split, r, &start, &len);
+        if (c < start + len) break;
+      }
+      float* to = P.out[which][r] + (c - start);
+      if (SBP_GUARD(to, 4)) *to = v;
+    } else {
+      const int n = P.replicas > 0 ? P.replicas : 1;
+      for (int r = 0; r < n; ++r) {
+        float* to = P.out[which][P.replicas > 0 ? r : z] + c;
+        if (SBP_GUARD(to, 4)) *to = v;
+      }
+    }
+  }
+}
+
+// Threads that share a row and chunks of eight elements each has, by the row's length; {0, 0}: the wide kernels.
+struct NormForm {
+  int g, nv;
+};
+NormForm norm_form(long long cols) {
+  if (cols <= 256) return {32, 1};
+  if (cols <= 512) return {32, 2};
+  if (cols <= 1024) return {128, 1};
+  if (cols <= 2048) return {128, 2};
+  if (cols <= 4096) return {256, 2};
+  if (cols <= 8192) return {512, 2};
+  if (cols <= 16384) return {512, 4};
+  return {0, 0};
+}
+
+// Blocks of a job: what the device holds, dealt out to the jobs, but no more than there are rows for.
+int norm_blocks(NormForm f, long long rows, int jobs, int per_sm) {
+  const long long most = (rows * (f.g ? f.g : kWide) + norm_threads(f.g ? f.g : kWide) - 1) / norm_threads(f.g ? f.g : kWide);
+  const long long fair = ((long long)device_sms() * per_sm + jobs - 1) / jobs;
+  return (int)(most < fair ? most : fair);
+}
+
+// Blocks an SM takes: forward as many threads as the registers of a row's elements, gamma and beta leave, backward of twice the sums.
+int blocks_per_sm(NormForm f, bool backward) {
+  if (!f.g) return backward ? 2 : 3;
+  const int threads = norm_threads(f.g);
+  return (backward ? (f.nv == 4 ? 512 : f.nv == 2 ? 512 : 1024) : (f.nv == 4 ? 512 : 1024)) / threads;
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+long long rows_of(const sbp_tensor* t, int r) {
+  int64_t shp[SBP_MAX_DIMS];
+  local_shape_nd(t, r, shp);
+  long long n = 1;
+  for (int d = 0; d + 1 < t->ndim; ++d) n *= shp[d];
+  return n;
+}
+
+bool is_float(int32_t dtype) { return dtype == SBP_F32 || dtype == SBP_BF16; }
+
+sbp_status check_rows(const sbp_tensor* t, const char* name, const sbp_tensor* like, bool need_ptrs) {
+  sbp_status st = check_tensor(t, name, need_ptrs);
+  if (st != SBP_OK) return st;
+  if (!is_float(t->dtype)) return fail(SBP_ERR_DTYPE, "%s must be F32 or BF16", name);
+  if (!like) {
+    if (t->ndim < 2) return fail(SBP_ERR_SHAPE, "%s needs at least two axes", name);
+    if (t->shape[t->ndim - 1] < 1) return fail(SBP_ERR_SHAPE, "%s: rows of no elements have no mean", name);
+    const sbp_sig s = t->sbp[0];
+    if (s.kind != SBP_SPLIT && s.kind != SBP_BROADCAST) return fail(SBP_ERR_SIGNATURE, "%s must be S(i) or B: normalising is not linear", name);
+    if (s.kind == SBP_SPLIT && s.axis == t->ndim - 1)
+      return fail(SBP_ERR_UNSUPPORTED, "%s is split along the axis that is normalised: box it to another signature first", name);
+    return SBP_OK;
+  }
+  if (placement_k(t) != placement_k(like)) return fail(SBP_ERR_INVALID_ARG, "%s and x differ in k", name);
+  if (t->ndim != like->ndim) return fail(SBP_ERR_SHAPE, "%s and x differ in shape", name);
+  for (int d = 0; d < t->ndim; ++d)
+    if (t->shape[d] != like->shape[d]) return fail(SBP_ERR_SHAPE, "%s and x differ in shape", name);
+  if (!same_sig(t->sbp[0], like->sbp[0])) return fail(SBP_ERR_SIGNATURE, "%s and x differ in signature", name);
+  return SBP_OK;
+}
+
+// mean or rstd
+sbp_status check_stat(const sbp_tensor* t, const char* name, const sbp_tensor* x) {
+  sbp_status st = check_tensor(t, name, true);
+  if (st != SBP_OK) return st;
+  if (t->dtype != SBP_F32) return fail(SBP_ERR_DTYPE, "%s must be F32", name);
+  if ((st = refuse_ld(t, name, "layer norm")) != SBP_OK) return st;
+  if (placement_k(t) != placement_k(x)) return fail(SBP_ERR_INVALID_ARG, "%s and x differ in k", name);
+  if (t->ndim != x->ndim - 1) return fail(SBP_ERR_SHAPE, "%s must have x's shape without its last axis", name);
+  for (int d = 0; d < t->ndim; ++d)
+    if (t->shape[d] != x->shape[d]) return fail(SBP_ERR_SHAPE, "%s must have x's shape without its last axis", name);
+  if (!same_sig(t->sbp[0], x->sbp[0])) return fail(SBP_ERR_SIGNATURE, "%s and x differ in signature", name);
+  return SBP_OK;
+}
+
+// gamma or beta
+sbp_status check_vector(const sbp_tensor* t, const char* name, const sbp_tensor* x) {
+  sbp_status st = check_tensor(t, name, true);
+  if (st != SBP_OK) return st;
+  if (!is_float(t->dtype)) return fail(SBP_ERR_DTYPE, "%s must be F32 or BF16", name);
+  if (placement_k(t) != placement_k(x)) return fail(SBP_ERR_INVALID_ARG, "%s and x differ in k", name);
+  if (t->ndim != 1 || t->shape[0] != x->shape[x->ndim - 1]) return fail(SBP_ERR_SHAPE, "%s must be [row length]", name);
+  if (t->sbp[0].kind != SBP_BROADCAST) return fail(SBP_ERR_SIGNATURE, "%s must be B", name);
+  return SBP_OK;
+}
+
+template <typename TX, typename TY, int G, int NV>
+cudaError_t launch_form(const NormParams& P, int jobs, int blocks, bool vec, bool backward, cudaStream_t st) {
+  const dim3 grid((unsigned)blocks, (unsigned)jobs), block(norm_threads(G));
+  if (backward)
+    return vec ? launch_dependent(norm_grad_kernel<TX, TY, G, NV, true>, grid, block, 0, st, P)
+               : launch_dependent(norm_grad_kernel<TX, TY, G, NV, false>, grid, block, 0, st, P);
+  return vec ? launch_dependent(norm_kernel<TX, TY, G, NV, true>, grid, block, 0, st, P)
+             : launch_dependent(norm_kernel<TX, TY, G, NV, false>, grid, block, 0, st, P);
+}
+
+template <typename TX, typename TY>
+cudaError_t launch_wide(const NormParams& P, int jobs, int blocks, bool vec, bool backward, cudaStream_t st) {
+  const dim3 grid((unsigned)blocks, (unsigned)jobs);
+  if (!backward)
+    return vec ? launch_dependent(norm_wide_kernel<TX, TY, true>, grid, dim3(kWide), 0, st, P)
+               : launch_dependent(norm_wide_kernel<TX, TY, false>, grid, dim3(kWide), 0, st, P);
+  const cudaError_t e = vec ? launch_dependent(norm_grad_wide_kernel<TX, TY, true>, grid, dim3(kWide), 0, st, P)
+                            : launch_dependent(norm_grad_wide_kernel<TX, TY, false>, grid, dim3(kWide), 0, st, P);
+  if (e != cudaSuccess || !P.parts) return e;
+  count_launch();
+  const dim3 cols((unsigned)((P.cols + 8 * kWideCols - 1) / (8 * kWideCols)), (unsigned)blocks, P.first_only ? 1u : (unsigned)jobs);
+  return vec ? launch_dependent(norm_sums_wide_kernel<TX, TY, true>, cols, dim3(kWideCols), 0, st, P)
+             : launch_dependent(norm_sums_wide_kernel<TX, TY, false>, cols, dim3(kWideCols), 0, st, P);
+}
+
+template <typename TX, typename TY>
+sbp_status launch_norm(const NormParams& P, int jobs, int blocks, bool backward, cudaStream_t st) {
+  bool vec = P.cols % 8 == 0;
+  for (int i = 0; i < jobs; ++i) {
+    const NormJob& j = P.j[i];
+    vec = vec && aligned16(j.x) && j.ldx * sizeof(TX) % 16 == 0 && aligned16(j.out) && j.ldo * (backward ? sizeof(TX) : sizeof(TY)) % 16 == 0;
+    if (backward) vec = vec && aligned16(j.dy) && j.lddy * sizeof(TY) % 16 == 0;
+  }
+  SBP_BOUNDS_UPLOAD(st);
+  const NormForm f = norm_form(P.cols);
+  cudaError_t e;
+  switch (f.g * 8 + f.nv) {
+    case 32 * 8 + 1: e = launch_form<TX, TY, 32, 1>(P, jobs, blocks, vec, backward, st); break;
+    case 32 * 8 + 2: e = launch_form<TX, TY, 32, 2>(P, jobs, blocks, vec, backward, st); break;
+    case 128 * 8 + 1: e = launch_form<TX, TY, 128, 1>(P, jobs, blocks, vec, backward, st); break;
+    case 128 * 8 + 2: e = launch_form<TX, TY, 128, 2>(P, jobs, blocks, vec, backward, st); break;
+    case 256 * 8 + 2: e = launch_form<TX, TY, 256, 2>(P, jobs, blocks, vec, backward, st); break;
+    case 512 * 8 + 2: e = launch_form<TX, TY, 512, 2>(P, jobs, blocks, vec, backward, st); break;
+    case 512 * 8 + 4: e = launch_form<TX, TY, 512, 4>(P, jobs, blocks, vec, backward, st); break;
+    default: e = launch_wide<TX, TY>(P, jobs, blocks, vec, backward, st); break;
+  }
+  if (e != cudaSuccess) return cuda_fail(e, "layer norm launch");
+  count_launch();
+  return SBP_OK;
+}
+
+// x_f32, y_f32: types of x (and its gradient) and of y (and its gradient)
+sbp_status launch_typed(const NormParams& P, int jobs, int blocks, bool backward, bool x_f32, bool y_f32, cudaStream_t st) {
+  if (jobs == 0) return SBP_OK;
+  using bf16 = __nv_bfloat16;
+  if (x_f32) return y_f32 ? launch_norm<float, float>(P, jobs, blocks, backward, st) : launch_norm<float, bf16>(P, jobs, blocks, backward, st);
+  return y_f32 ? launch_norm<bf16, float>(P, jobs, blocks, backward, st) : launch_norm<bf16, bf16>(P, jobs, blocks, backward, st);
+}
+
+// Blocks a job gets in the backward pass of x, and the jobs whose sums the workspace holds: the same for the query and the call.
+int backward_blocks(const sbp_tensor* x, int* jobs) {
+  const NormForm f = norm_form(x->shape[x->ndim - 1]);
+  long long most = 0;
+  *jobs = 0;
+  for (int r = 0; r < placement_k(x); ++r) {
+    const long long n = rows_of(x, r);
+    most = n > most ? n : most;
+    if (n > 0) ++*jobs;
+  }
+  if (*jobs && x->sbp[0].kind == SBP_BROADCAST) *jobs = 1;
+  return *jobs ? norm_blocks(f, most, *jobs, blocks_per_sm(f, true)) : 0;
+}
+
+}  // namespace
+
+}  // namespace sbp
+
+using namespace sbp;
+
+extern "C" {
+
+sbp_status sbp_layer_norm(const sbp_tensor* x, const sbp_tensor* gamma, const sbp_tensor* beta, sbp_tensor* y, sbp_tensor* mean,
+                          sbp_tensor* rstd, float eps, void* cuda_stream) {
+  SBP_RANGE("sbp_layer_norm");
+  sbp_status st = check_rows(x, "x", nullptr, true);
+  if (st != SBP_OK) return st;
+  if ((st = check_rows(y, "y", x, true)) != SBP_OK) return st;
+  if (gamma && (st = check_vector(gamma, "gamma", x)) != SBP_OK) return st;
+  if (beta && (st = check_vector(beta, "beta", x)) != SBP_OK) return st;
+  if (mean && (st = check_stat(mean, "mean", x)) != SBP_OK) return st;
+  if (rstd && (st = check_stat(rstd, "rstd", x)) != SBP_OK) return st;
+  if (!(eps >= 0.f) || eps > 3.4e38f) return fail(SBP_ERR_INVALID_ARG, "eps must be finite and not negative");
+  if (x->shape[x->ndim - 1] > (1LL << 31)) return fail(SBP_ERR_UNSUPPORTED, "rows of more than 2^31 elements");
+  NormParams P{};
+  P.gamma = gamma ? gamma->local[0] : nullptr;
+  P.beta = beta ? beta->local[0] : nullptr;
+  P.gamma_f32 = gamma && gamma->dtype == SBP_F32;
+  P.beta_f32 = beta && beta->dtype == SBP_F32;
+  P.cols = x->shape[x->ndim - 1];
+  P.eps = eps;
+  int n = 0;
+  long long most = 0;
+  for (int r = 0; r < placement_k(x); ++r) {
+    NormJob j{};
+    j.rows = rows_of(x, r);
+    if (j.rows == 0) continue;
+    j.x = x->local[r];
+    j.ldx = local_pitch(x, r);
+    j.out = y->local[r];
+    j.ldo = local_pitch(y, r);
+    j.mean = mean ? static_cast<float*>(mean->local[r]) : nullptr;
+    j.rstd = rstd ? static_cast<float*>(rstd->local[r]) : nullptr;
+    bool seen = false;
+    for (int i = 0; i < n; ++i) seen = seen || (P.j[i].out == j.out && P.j[i].mean == j.mean && P.j[i].rstd == j.rstd);
+    if (seen && x->sbp[0].kind == SBP_BROADCAST) continue;
+    P.j[n++] = j;
+    most = j.rows > most ? j.rows : most;
+  }
+  SBP_BOUNDS_RESET();
+  SBP_BOUNDS_TENSOR(x);
+  SBP_BOUNDS_TENSOR(gamma);
+  SBP_BOUNDS_TENSOR(beta);
+  SBP_BOUNDS_TENSOR(y);
+  SBP_BOUNDS_TENSOR(mean);
+  SBP_BOUNDS_TENSOR(rstd);
+  const NormForm f = norm_form(P.cols);
+  return launch_typed(P, n, n ? norm_blocks(f, most, n, blocks_per_sm(f, false)) : 0, false, x->dtype == SBP_F32, y->dtype == SBP_F32,
+                      static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t sbp_layer_norm_backward_workspace_bytes(const sbp_tensor* x) {
+  if (check_rows(x, "x", nullptr, false) != SBP_OK) return 0;
+  int jobs = 0;
+  const int blocks = backward_blocks(x, &jobs);
+  return (size_t)blocks * jobs * 2 * (size_t)x->shape[x->ndim - 1] * sizeof(float);
+}
+
+sbp_status sbp_layer_norm_backward(const sbp_tensor* x, const sbp_tensor* gamma, const sbp_tensor* mean, const sbp_tensor* rstd,
+                                   const sbp_tensor* grad_y, sbp_tensor* grad_x, sbp_tensor* grad_gamma, sbp_tensor* grad_beta, void* ws,
+                                   size_t ws_bytes, void* cuda_stream) {
+  SBP_RANGE("sbp_layer_norm_backward");
+  sbp_status st = check_rows(x, "x", nullptr, true);
+  if (st != SBP_OK) return st;
+  if ((st = check_rows(grad_y, "grad_y", x, true)) != SBP_OK) return st;
+  if ((st = check_rows(grad_x, "grad_x", x, true)) != SBP_OK) return st;
+  if (grad_x->dtype != x->dtype) return fail(SBP_ERR_DTYPE, "grad_x must have x's dtype");
+  if (gamma && (st = check_vector(gamma, "gamma", x)) != SBP_OK) return st;
+  if ((st = check_stat(mean, "mean", x)) != SBP_OK) return st;
+  if ((st = check_stat(rstd, "rstd", x)) != SBP_OK) return st;
+  const int k = placement_k(x);
+  const bool x_b = x->sbp[0].kind == SBP_BROADCAST;
+  sbp_tensor* const grads[2] = {grad_gamma, grad_beta};
+  const char* const names[2] = {"grad_gamma", "grad_beta"};
+  sbp_sig sig{SBP_BROADCAST, 0};
+  bool wanted = false;
+  for (int i = 0; i < 2; ++i) {
+    const sbp_tensor* t = grads[i];
+    if (!t) continue;
+    if ((st = check_tensor(t, names[i], true)) != SBP_OK) return st;
+    if (t->dtype != SBP_F32) return fail(SBP_ERR_DTYPE, "%s must be F32", names[i]);
+    if (placement_k(t) != k) return fail(SBP_ERR_INVALID_ARG, "%s and x differ in k", names[i]);
+    if (t->ndim != 1 || t->shape[0] != x->shape[x->ndim - 1]) return fail(SBP_ERR_SHAPE, "%s must be [row length]", names[i]);
+    const sbp_sig s = t->sbp[0];
+    if (s.kind == SBP_PARTIAL_MAX || (s.kind == SBP_PARTIAL_SUM && x_b))
+      return fail(SBP_ERR_SIGNATURE, "%s must be %sB or S(0)", names[i], x_b ? "" : "P(sum), ");
+    if (wanted && !same_sig(s, sig)) return fail(SBP_ERR_SIGNATURE, "grad_gamma and grad_beta differ in signature");
+    sig = s;
+    wanted = true;
+  }
+  if (x->shape[x->ndim - 1] > (1LL << 31)) return fail(SBP_ERR_UNSUPPORTED, "rows of more than 2^31 elements");
+  int jobs_most = 0;
+  const int blocks = backward_blocks(x, &jobs_most);
+  const size_t need = sbp_layer_norm_backward_workspace_bytes(x);
+  if (wanted && need > 0) {
+    if (!ws || ws_bytes < need) return fail(SBP_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, ws_bytes);
+    if (!aligned16(ws)) return fail(SBP_ERR_ALIGNMENT, "workspace must be 16-byte aligned");
+  }
+
+  NormParams P{};
+  P.gamma = gamma ? gamma->local[0] : nullptr;
+  P.gamma_f32 = gamma && gamma->dtype == SBP_F32;
+  P.cols = x->shape[x->ndim - 1];
+  P.parts = wanted ? static_cast<float*>(ws) : nullptr;
+  P.first_only = x_b;
+  JoinParams Q{};
+  int n = 0;
+  for (int r = 0; r < k; ++r) {
+    NormJob j{};
+    j.rows = rows_of(x, r);
+    Q.lo[r] = Q.hi[r] = n;
+    if (j.rows == 0) continue;
+    j.x = x->local[r];
+    j.ldx = local_pitch(x, r);
+    j.dy = grad_y->local[r];
+    j.lddy = local_pitch(grad_y, r);
+    j.out = grad_x->local[r];
+    j.ldo = local_pitch(grad_x, r);
+    j.mean = static_cast<float*>(mean->local[r]);
+    j.rstd = static_cast<float*>(rstd->local[r]);
+    bool seen = false;
+    for (int i = 0; i < n; ++i) seen = seen || P.j[i].out == j.out;
+    if (seen && x_b) continue;
+    P.j[n++] = j;
+    Q.hi[r] = n;
+  }
+  SBP_BOUNDS_RESET();
+  SBP_BOUNDS_TENSOR(x);
+  SBP_BOUNDS_TENSOR(gamma);
+  SBP_BOUNDS_TENSOR(mean);
+  SBP_BOUNDS_TENSOR(rstd);
+  SBP_BOUNDS_TENSOR(grad_y);
+  SBP_BOUNDS_TENSOR(grad_x);
+  SBP_BOUNDS_TENSOR(grad_gamma);
+  SBP_BOUNDS_TENSOR(grad_beta);
+  SBP_BOUNDS_ADD(ws, ws_bytes);
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  st = launch_typed(P, n, blocks, true, x->dtype == SBP_F32, grad_y->dtype == SBP_F32, stream);
+  if (st != SBP_OK || !wanted) return st;
+
+  Q.parts = P.parts;
+  Q.cols = P.cols;
+  Q.per_job = blocks;
+  const bool partial = sig.kind == SBP_PARTIAL_SUM;
+  if (!partial) {                // every row once: of a B tensor those of one replica
+    Q.lo[0] = 0;
+    Q.hi[0] = x_b ? (n > 0 ? 1 : 0) : n;
+  }
+  for (int i = 0; i < 2; ++i) {
+    if (!grads[i]) continue;
+    for (int r = 0; r < k; ++r) Q.out[i][r] = static_cast<float*>(grads[i]->local[r]);
+  }
+  if (sig.kind == SBP_SPLIT) Q.split = k;
+  if (sig.kind == SBP_BROADCAST) Q.replicas = k;
+  const dim3 grid((unsigned)((P.cols + 31) / 32), 2, partial ? (unsigned)k : 1u);
+  SBP_BOUNDS_UPLOAD(stream);
+  const cudaError_t e = launch_dependent(norm_join_kernel, grid, dim3(256), 0, stream, Q);
+  if (e != cudaSuccess) return cuda_fail(e, "layer norm gradient launch");
+  count_launch();
+  return SBP_OK;
+}
+
+}  // extern "C"

@@ -9,6 +9,7 @@
 //     workspace was given for, one such chain.
 #include <cuda_bf16.h>
 
+#include "blocks8.h"
 #include "bounds_check.h"
 #include "matmul_plan.h"
 #include "sbp_internal.h"
@@ -336,12 +337,12 @@ static bool is_s(sbp_sig s, int ax) { return s.kind == SBP_SPLIT && s.axis == ax
 static bool is_b(sbp_sig s) { return s.kind == SBP_BROADCAST; }
 static bool is_p(sbp_sig s) { return s.kind == SBP_PARTIAL_SUM; }
 
-// Validates the three descriptors and fills the plan.  need_ptrs = false for size queries.
-static sbp_status build_plan(const sbp_tensor* x, const sbp_tensor* w, const sbp_tensor* y, uint32_t flags,
-                             bool need_ptrs, MatmulPlan* plan) {
-  sbp_status st = check_tensor(x, "x", need_ptrs);
+// Validates the three descriptors and fills the plan.  need_ptrs = false for size queries; eight: x and w are E4M3 values.
+sbp_status build_matmul_plan(const sbp_tensor* x, const sbp_tensor* w, const sbp_tensor* y, uint32_t flags, bool need_ptrs, bool eight,
+                             MatmulPlan* plan) {
+  sbp_status st = eight ? check_tensor8(x, "x", need_ptrs) : check_tensor(x, "x", need_ptrs);
   if (st != SBP_OK) return st;
-  st = check_tensor(w, "w", need_ptrs);
+  st = eight ? check_tensor8(w, "w", need_ptrs) : check_tensor(w, "w", need_ptrs);
   if (st != SBP_OK) return st;
   st = check_tensor(y, "y", need_ptrs);
   if (st != SBP_OK) return st;
@@ -354,7 +355,8 @@ static sbp_status build_plan(const sbp_tensor* x, const sbp_tensor* w, const sbp
     return fail(SBP_ERR_SHAPE, "x is [%lld,%lld] but w has %lld rows", M, K, (long long)w->shape[tw ? 1 : 0]);
   if (y->shape[0] != M || y->shape[1] != N) return fail(SBP_ERR_SHAPE, "y must be [%lld,%lld]", M, N);
   if (x->dtype != w->dtype) return fail(SBP_ERR_DTYPE, "x and w differ in dtype");
-  if (x->dtype != SBP_F32 && x->dtype != SBP_BF16) return fail(SBP_ERR_DTYPE, "operands must be F32 or BF16");
+  if (eight && x->dtype != SBP_E4M3) return fail(SBP_ERR_DTYPE, "operands must be E4M3");
+  if (!eight && x->dtype != SBP_F32 && x->dtype != SBP_BF16) return fail(SBP_ERR_DTYPE, "operands must be F32 or BF16");
   if (y->dtype != SBP_F32 && y->dtype != SBP_BF16) return fail(SBP_ERR_DTYPE, "y must be F32 or BF16");
   if (x->dtype == SBP_F32 && y->dtype != SBP_F32) return fail(SBP_ERR_DTYPE, "F32 operands need an F32 result");
   const int k = placement_k(x);
@@ -453,6 +455,11 @@ static sbp_status build_plan(const sbp_tensor* x, const sbp_tensor* w, const sbp
     }
   }
   return SBP_OK;
+}
+
+static sbp_status build_plan(const sbp_tensor* x, const sbp_tensor* w, const sbp_tensor* y, uint32_t flags, bool need_ptrs,
+                             MatmulPlan* plan) {
+  return build_matmul_plan(x, w, y, flags, need_ptrs, false, plan);
 }
 
 // Two-axis placements (Section 3.3, Table 3): Table 1 is applied to each placement axis on its

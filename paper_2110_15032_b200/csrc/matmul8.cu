@@ -1,0 +1,752 @@
+// MatMul of 8-bit blocks: executes a grouped-GEMM plan (matmul_plan.h) whose operands are e4m3 values with a scale for each block of
+// 128 along the contraction, both stored with the contraction last.
+//
+// A ring slot is one block: rows of 128 bytes are exactly what the 128-byte swizzle holds.  Four tcgen05.mma of K = 32 make the
+// block's sum in tensor memory; the accumulating warps multiply it by the block's two scales and add it to fp32 registers while
+// the next block's products go to another part of tensor memory.  So any fp32 scale is taken, and what the tensor cores add up
+// unscaled is never more than 128 products.
+//
+//   warps 0-7    the accumulators: 32 rows x half of the tile's columns each, a row a thread
+//   warp 8       operands by bulk tensor copies (TMA form)
+//   warp 9       one elected lane issues the MMAs
+//   warps 10-11  the scales of a block into a ring of their own, asynchronously
+//   warps 12-15  operands by plain loads, where base or pitch is not a multiple of 16 bytes (the other form)
+//
+// Forms: a CTA pair with 256 x 256 tiles, persistent; single CTAs with 128 x NB tiles, cut along the contraction over a cluster where
+// there are few of them.  Few rows (columns): the 128 rows of the tile are the other operand's.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "blocks8.h"
+#include "bounds_check.h"
+#include "matmul_plan.h"
+#include "sbp_internal.h"
+#include "tc_ptx.h"
+
+namespace sbp {
+
+// Defined in matmul.cu and matmul_tc.cu.
+sbp_status build_matmul_plan(const sbp_tensor* x, const sbp_tensor* w, const sbp_tensor* y, uint32_t flags, bool need_ptrs, bool eight,
+                             MatmulPlan* plan);
+bool tensor_map8(CUtensorMap* map, const void* base, long long rows, long long cols, long long ld, int box_rows);
+
+namespace {
+
+constexpr int kRows = 128;                   // rows of the A operand a CTA holds
+constexpr int kRing = 168 * 1024;
+constexpr int kScaleSlots = 8;
+constexpr int kSlab = 32 * 128;              // staging of an accumulating warp: 32 rows of 128 bytes
+constexpr int kAccWarps = 8;
+constexpr int kPanel = 8;                    // row tiles walked together
+
+struct Params8 {
+  CUtensorMap map_a[SBP_MAX_K], map_b[SBP_MAX_K];
+  // as stored, for the loading form: bases, pitches and K of every segment
+  const unsigned char* a[SBP_MAX_K];
+  const unsigned char* b[SBP_MAX_K];
+  long long lda[SBP_MAX_K], ldb[SBP_MAX_K], kseg[SBP_MAX_K];
+  const float* sa[SBP_MAX_K];
+  const float* sb[SBP_MAX_K];
+  int kblocks[SBP_MAX_K];                    // per segment; also the pitch of its scales
+  long long m[SBP_MAX_K], n[SBP_MAX_K], row_off[SBP_MAX_K], col_off[SBP_MAX_K], ldy[SBP_MAX_K];
+  void* y[SBP_MAX_K];
+  void* y_rep[SBP_MAX_K];
+  int tile_begin[SBP_MAX_K + 1], tiles_m[SBP_MAX_K], tiles_n[SBP_MAX_K];
+  int n_rep, ngroups, nseg, chain, total_tiles;
+  int a_tiles, b_tiles;                      // the scales are one for 128 rows (columns)
+  int per_column;                            // a scale a column, else one for 128 columns of a tile
+  int out_f32, swap;                         // swap: rows of the tile are columns of the result
+  int splits;                                // CTAs of a cluster that share a tile's contraction
+};
+
+constexpr unsigned idesc8(int rows, int cols) { return (1u << 4) | ((unsigned)(cols >> 3) << 17) | ((unsigned)(rows >> 4) << 24); }
+
+template <bool PAIR>
+__device__ __forceinline__ void umma8(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate) {
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+__device__ __forceinline__ void tma_load_cta(unsigned dst, const CUtensorMap* map, int x, int y, unsigned bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+               "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
+
+// N accumulator columns of this warp's 32 rows, in pairs
+template <int N>
+__device__ __forceinline__ void tmem_pairs(unsigned taddr, unsigned long long* v) {
+  float f[N];
+  if constexpr (N == 32) tmem_ld32(taddr, f);
+  else {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) tmem_ld8(taddr + i, f + i);
+  }
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) asm volatile("mov.b64 %0, {%1, %2};" : "=l"(v[i]) : "f"(f[2 * i]), "f"(f[2 * i + 1]));
+}
+__device__ __forceinline__ unsigned long long two8(float x, float y) {
+  unsigned long long v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+  return v;
+}
+__device__ __forceinline__ float lo8(unsigned long long v) { return __uint_as_float((unsigned)v); }
+__device__ __forceinline__ float hi8(unsigned long long v) { return __uint_as_float((unsigned)(v >> 32)); }
+
+template <bool PAIR, int NB, bool TMA>
+struct Shape8 {
+  static constexpr int kColsCta = PAIR ? NB / 2 : NB;            // B rows this CTA loads
+  static constexpr int kSlot = (kRows + kColsCta) * 128;
+  static constexpr int kSlots = kRing / kSlot;                   // 5 (256 and 128 columns), 7, 8, 9
+  static constexpr int kAccs = NB == 256 ? 2 : 4, kAccCols = NB == 256 ? 256 : 128;
+  static constexpr int kScales = kRows + NB;                     // floats of a block
+  static constexpr int kThreads = TMA ? 384 : 512;
+  static constexpr int kSmem = kSlots * kSlot + kAccWarps * kSlab + kScaleSlots * kScales * 4 + 1024;
+};
+
+struct Tile8 {
+  int g, m0, n0;
+};
+__device__ __forceinline__ Tile8 tile_at(const Params8& p, int tile, int tm, int tn) {
+  int g = 0;
+  while (g + 1 < p.ngroups && tile >= p.tile_begin[g + 1]) ++g;
+  const int t = tile - p.tile_begin[g], panel_tiles = kPanel * p.tiles_n[g];
+  const int panel = t / panel_tiles, r = t - panel * panel_tiles;
+  const int high = min(kPanel, p.tiles_m[g] - panel * kPanel);
+  const int n = r / high;
+  return {g, (panel * kPanel + (r - n * high)) * tm, n * tn};
+}
+
+// The blocks of a tile, or of one CTA's share of it: segment, block inside it, how many.
+struct Run8 {
+  int s, kb, count;
+};
+__device__ __forceinline__ Run8 blocks_of(const Params8& p, int g, int slice) {
+  const int s_lo = p.chain ? 0 : g, s_hi = p.chain ? p.nseg : g + 1;
+  int total = 0;
+  for (int s = s_lo; s < s_hi; ++s) total += p.kblocks[s];
+  const int first = (int)((long long)total * slice / p.splits);
+  Run8 r{s_lo, first, (int)((long long)total * (slice + 1) / p.splits) - first};
+  while (r.s + 1 < s_hi && r.kb >= p.kblocks[r.s]) r.kb -= p.kblocks[r.s++];
+  return r;
+}
+__device__ __forceinline__ void next_block(const Params8& p, Run8& r) {
+  if (++r.kb < p.kblocks[r.s] || !p.chain) return;
+  r.kb = 0;
+  do ++r.s;
+  while (r.s + 1 < p.nseg && p.kblocks[r.s] == 0);
+}
+
+// 16 bytes of a row from byte k on, zeros past `len`; the row may start anywhere.
+__device__ __forceinline__ uint4 row_bytes(const unsigned char* row, long long k, long long len) {
+  const unsigned char* at = row + k;
+  const unsigned off = (unsigned)(reinterpret_cast<unsigned long long>(at) & 3);
+  if (k + 20 <= len && (off == 0 || k >= 4)) {      // five aligned words inside the row
+    const unsigned* w = reinterpret_cast<const unsigned*>(at - off);
+    unsigned v[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) v[i] = SBP_GUARD(w + i, 4) ? w[i] : 0u;
+    return make_uint4(__funnelshift_r(v[0], v[1], off * 8), __funnelshift_r(v[1], v[2], off * 8), __funnelshift_r(v[2], v[3], off * 8),
+                      __funnelshift_r(v[3], v[4], off * 8));
+  }
+  unsigned v[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (k + i < len && SBP_GUARD(at + i, 1)) v[i >> 2] |= (unsigned)at[i] << (8 * (i & 3));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+__device__ __forceinline__ void store_one(const Params8& p, void* y, long long at, float v) {
+  if (p.out_f32) {
+    float* to = static_cast<float*>(y) + at;
+    if (SBP_GUARD(to, 4)) *to = v;
+  } else {
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(y) + at;
+    if (SBP_GUARD(to, 2)) *to = __float2bfloat16_rn(v);
+  }
+}
+
+template <bool PAIR, int NB, bool TMA>
+__global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_kernel(const __grid_constant__ Params8 p) {
+  using C = Shape8<PAIR, NB, TMA>;
+  constexpr int kHalf = NB / 2;                    // columns of an accumulating warp
+  constexpr int kTileM = PAIR ? 256 : 128;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) unsigned long long bar_full[C::kSlots], bar_empty[C::kSlots], bar_acc_full[C::kAccs], bar_acc_empty[C::kAccs],
+      bar_sc_full[kScaleSlots], bar_sc_empty[kScaleSlots];
+  __shared__ unsigned tmem_base_slot;
+  __shared__ int abort_flag_s;
+  volatile int* abort_flag = &abort_flag_s;
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  unsigned char* staging = smem + C::kSlots * C::kSlot;
+  float* scales = reinterpret_cast<float*>(staging + kAccWarps * kSlab);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const unsigned rank = PAIR ? cluster_ctarank() : 0u;
+
+  if (tid == 0) {
+    abort_flag_s = 0;
+    for (int i = 0; i < C::kSlots; ++i) {
+      mbar_init(smem_addr(&bar_full[i]), TMA ? 1 : 4);      // PAIR: used in CTA 0, with both CTAs' bytes
+      mbar_init(smem_addr(&bar_empty[i]), 1);
+    }
+    for (int i = 0; i < C::kAccs; ++i) {
+      mbar_init(smem_addr(&bar_acc_full[i]), 1);
+      mbar_init(smem_addr(&bar_acc_empty[i]), (PAIR ? 2 : 1) * kAccWarps);      // PAIR: used in CTA 0
+    }
+    for (int i = 0; i < kScaleSlots; ++i) {
+      mbar_init(smem_addr(&bar_sc_full[i]), 64);
+      mbar_init(smem_addr(&bar_sc_empty[i]), kAccWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 9) {
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_slot)), "r"(512) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_slot)), "r"(512) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  if constexpr (PAIR) cluster_sync_all();
+  else __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const unsigned tmem_base = tmem_base_slot;
+  SBP_PDL_RELEASE();
+  SBP_PDL_WAIT();
+
+  const int splits = PAIR ? 1 : p.splits, slice = PAIR ? 0 : (int)(blockIdx.x % (unsigned)p.splits);
+  const int first = PAIR ? (int)(blockIdx.x >> 1) : (int)(blockIdx.x / (unsigned)p.splits);
+  const int stride = PAIR ? (int)(gridDim.x >> 1) : (int)(gridDim.x / (unsigned)p.splits);
+
+  if (warp < kAccWarps) {
+    // ------------------------------------------------ accumulators
+    if constexpr (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");      // 2 x 216 + 72 = 3 x 168
+    const int q = warp & 3, half = warp >> 2;
+    const int row = q * 32 + lane;                 // of this CTA's 128
+    const unsigned acc_empty0 = PAIR ? map_to_cta(smem_addr(&bar_acc_empty[0]), 0) : smem_addr(&bar_acc_empty[0]);
+    int a = 0, ss = 0;
+    unsigned a_round = 0, s_round = 0;
+    bool ok = true;
+    for (int tile = first; tile < p.total_tiles && ok; tile += stride) {
+      const Tile8 tc = tile_at(p, tile, kTileM, NB);
+      const int count = blocks_of(p, tc.g, slice).count;
+      unsigned long long acc[NB / 4];
+#pragma unroll
+      for (int i = 0; i < NB / 4; ++i) acc[i] = 0ull;
+      for (int c = 0; c < count; ++c) {
+        ok = mbar_wait_warp(smem_addr(&bar_sc_full[ss]), s_round, abort_flag);
+        if (!ok) break;
+        const float* sc = scales + ss * C::kScales;
+        const float rs = sc[row];
+        ok = mbar_wait_warp(smem_addr(&bar_acc_full[a]), a_round, abort_flag);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + half * kHalf;
+        constexpr int kStep = kHalf < 32 ? kHalf : 32;
+        if (!p.per_column) {
+          const float s = rs * sc[kRows + (NB == 256 ? half : 0)];
+          const unsigned long long s2 = two8(s, s);
+#pragma unroll
+          for (int b = 0; b < kHalf; b += kStep) {
+            unsigned long long v[kStep / 2];
+            tmem_pairs<kStep>(at + b, v);
+#pragma unroll
+            for (int i = 0; i < kStep / 2; ++i) asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[b / 2 + i]) : "l"(v[i]), "l"(s2));
+          }
+        } else {
+          const unsigned long long r2 = two8(rs, rs);
+          const float* cs = sc + kRows + half * kHalf;
+#pragma unroll
+          for (int b = 0; b < kHalf; b += kStep) {
+            unsigned long long v[kStep / 2];
+            tmem_pairs<kStep>(at + b, v);
+#pragma unroll
+            for (int i = 0; i < kStep / 2; i += 2) {
+              const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(cs + b + 2 * i);
+              asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v[i]) : "l"(s.x));
+              asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v[i + 1]) : "l"(s.y));
+              asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[b / 2 + i]) : "l"(v[i]), "l"(r2));
+              asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[b / 2 + i + 1]) : "l"(v[i + 1]), "l"(r2));
+            }
+          }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (PAIR) mbar_arrive_cluster(acc_empty0 + a * 8);
+          else mbar_arrive(acc_empty0 + a * 8);
+          mbar_arrive(smem_addr(&bar_sc_empty[ss]));
+        }
+        if (++a == C::kAccs) { a = 0; a_round ^= 1; }
+        if (++ss == kScaleSlots) { ss = 0; s_round ^= 1; }
+      }
+      if (!ok) break;
+      const long long M = p.m[tc.g], N = p.n[tc.g], ldy = p.ldy[tc.g];
+      const int n_out = (tc.g == 0 ? p.n_rep : 0) + 1;
+      const long long row0 = tc.m0 + (int)rank * kRows, col0 = tc.n0 + half * kHalf;
+      if (splits > 1) {                            // the partial tile, for the cluster to add up; the ring is done with
+        float* mine = reinterpret_cast<float*>(smem) + row * (NB + 1) + half * kHalf;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < kHalf / 2; ++i) {
+          mine[2 * i] = lo8(acc[i]);
+          mine[2 * i + 1] = hi8(acc[i]);
+        }
+      } else if (p.swap) {                         // neighbouring lanes are neighbouring columns of the result
+        const long long n = row0 + row;
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+          const float v = i & 1 ? hi8(acc[i / 2]) : lo8(acc[i / 2]);
+          if (n < M && col0 + i < N)
+            for (int o = 0; o < n_out; ++o) store_one(p, o == 0 ? p.y[tc.g] : p.y_rep[o - 1], (col0 + i) * ldy + n, v);
+        }
+      } else {
+        // through a slab of shared memory, so that a warp stores whole pieces of rows
+        unsigned char* slab = staging + warp * kSlab;
+        auto rows_out = [&](auto f32_tag) {
+          constexpr bool F32 = decltype(f32_tag)::value;
+          constexpr int esz = F32 ? 4 : 2, kCols = kHalf < 128 / esz ? kHalf : 128 / esz, kChunks = kCols * esz / 16;
+          constexpr int kPer = 16 / esz;           // elements of a 16-byte chunk
+          bool vec = ldy * esz % 16 == 0;
+          for (int o = 0; o < n_out; ++o) vec = vec && (reinterpret_cast<unsigned long long>(o == 0 ? p.y[tc.g] : p.y_rep[o - 1]) & 15) == 0;
+#pragma unroll
+          for (int s = 0; s < kHalf / kCols; ++s) {
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+              const unsigned long long* f = acc + (s * kCols + c * kPer) / 2;
+              uint4 o;
+              if constexpr (F32) o = make_uint4((unsigned)f[0], (unsigned)(f[0] >> 32), (unsigned)f[1], (unsigned)(f[1] >> 32));
+              else o = make_uint4(bf16_two(lo8(f[0]), hi8(f[0])), bf16_two(lo8(f[1]), hi8(f[1])), bf16_two(lo8(f[2]), hi8(f[2])), bf16_two(lo8(f[3]), hi8(f[3])));
+              *reinterpret_cast<uint4*>(slab + lane * 128 + ((c ^ (lane & 7)) << 4)) = o;
+            }
+            __syncwarp();
+            for (int i = 0; i < kChunks; ++i) {
+              const int r = i * (32 / kChunks) + lane / kChunks, c = lane % kChunks;
+              const long long m = row0 + q * 32 + r, n = col0 + s * kCols + c * kPer;
+              if (m >= M || n >= N) continue;
+              const unsigned char* from = slab + r * 128 + ((c ^ (r & 7)) << 4);
+              for (int o = 0; o < n_out; ++o) {
+                unsigned char* to = static_cast<unsigned char*>(o == 0 ? p.y[tc.g] : p.y_rep[o - 1]) + (m * ldy + n) * esz;
+                if (vec && n + kPer <= N) {
+                  if (SBP_GUARD(to, 16)) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+                } else {
+                  for (int e = 0; e < kPer && n + e < N; ++e) {
+                    if (!SBP_GUARD(to + e * esz, esz)) continue;
+                    if constexpr (F32) *reinterpret_cast<float*>(to + e * 4) = *reinterpret_cast<const float*>(from + e * 4);
+                    else *reinterpret_cast<unsigned short*>(to + e * 2) = *reinterpret_cast<const unsigned short*>(from + e * 2);
+                  }
+                }
+              }
+            }
+          }
+        };
+        if (p.out_f32) rows_out(std::true_type{});
+        else rows_out(std::false_type{});
+      }
+    }
+  } else {
+    if constexpr (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 8 && TMA) {
+      // ------------------------------------------------ operands, by the copy engine
+      const bool leader = elect_one();
+      int slot = 0;
+      unsigned round = 0;
+      long long issued = 0;
+      bool ok = true;
+      for (int tile = first; tile < p.total_tiles && ok; tile += stride) {
+        const Tile8 tc = tile_at(p, tile, kTileM, NB);
+        Run8 run = blocks_of(p, tc.g, slice);
+        const int arow = (int)p.row_off[tc.g] + tc.m0 + (int)rank * kRows, brow = (int)p.col_off[tc.g] + tc.n0 + (int)rank * C::kColsCta;
+        for (int c = 0; c < run.count; ++c) {
+          ok = mbar_wait_warp(smem_addr(&bar_empty[slot]), round ^ 1, abort_flag);
+          if (!ok) break;
+          if (leader) {
+            const unsigned sa = smem_addr(smem + slot * C::kSlot), sb = sa + kRows * 128;
+            if constexpr (PAIR) {
+              const unsigned full0 = map_to_cta(smem_addr(&bar_full[slot]), 0);
+              if (rank == 0) mbar_expect_tx(smem_addr(&bar_full[slot]), 2 * C::kSlot);
+              tma_load_2d(sa, &p.map_a[run.s], run.kb * 128, arow, full0);
+              tma_load_2d(sb, &p.map_b[run.s], run.kb * 128, brow, full0);
+            } else {
+              mbar_expect_tx(smem_addr(&bar_full[slot]), C::kSlot);
+              tma_load_cta(sa, &p.map_a[run.s], run.kb * 128, arow, smem_addr(&bar_full[slot]));
+              tma_load_cta(sb, &p.map_b[run.s], run.kb * 128, brow, smem_addr(&bar_full[slot]));
+            }
+          }
+          __syncwarp();
+          ++issued;
+          if (++slot == C::kSlots) { slot = 0; round ^= 1; }
+          next_block(p, run);
+        }
+      }
+      if (*abort_flag && rank == 0 && leader) {    // loads in flight get a bounded chance to land
+        for (long long i = issued > C::kSlots ? issued - C::kSlots : 0; i < issued; ++i) {
+          const unsigned long long t0 = now_ns();
+          while (!mbar_try(smem_addr(&bar_full[i % C::kSlots]), (unsigned)((i / C::kSlots) & 1)) && now_ns() - t0 < 100000000ull) {
+          }
+        }
+      }
+    } else if (warp == 9) {
+      // ------------------------------------------------ MMA issuer (PAIR: the first CTA's)
+      if (rank == 0) {
+        const bool leader = elect_one();
+        int slot = 0, a = 0;
+        unsigned round = 0, a_round = 0;
+        constexpr unsigned idesc = idesc8(kTileM, NB), lo = desc_lo_fixed(16), hi = desc_hi_fixed(1024);
+        bool ok = true;
+        for (int tile = first; tile < p.total_tiles && ok; tile += stride) {
+          const Tile8 tc = tile_at(p, tile, kTileM, NB);
+          const int count = blocks_of(p, tc.g, slice).count;
+          for (int c = 0; c < count; ++c) {
+            ok = mbar_wait_warp(smem_addr(&bar_acc_empty[a]), a_round ^ 1, abort_flag) && mbar_wait_warp(smem_addr(&bar_full[slot]), round, abort_flag);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (leader) {
+              const unsigned sa = smem_addr(smem + slot * C::kSlot), sb = sa + kRows * 128;
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)       // 32 bytes of every row
+                umma8<PAIR>(tmem_base + a * C::kAccCols, desc_pack(lo + (sa >> 4) + kk * 2, hi), desc_pack(lo + (sb >> 4) + kk * 2, hi), idesc,
+                            kk == 0 ? 0u : 1u);
+              if constexpr (PAIR) {
+                umma_commit_pair(smem_addr(&bar_empty[slot]));
+                umma_commit_pair(smem_addr(&bar_acc_full[a]));
+              } else {
+                umma_commit_cta(smem_addr(&bar_empty[slot]));
+                umma_commit_cta(smem_addr(&bar_acc_full[a]));
+              }
+            }
+            __syncwarp();
+            if (++slot == C::kSlots) { slot = 0; round ^= 1; }
+            if (++a == C::kAccs) { a = 0; a_round ^= 1; }
+          }
+        }
+      }
+    } else if (warp == 10 || warp == 11) {
+      // ------------------------------------------------ scales
+      const int t = tid - 320;
+      int ss = 0;
+      unsigned round = 0;
+      bool ok = true;
+      for (int tile = first; tile < p.total_tiles && ok; tile += stride) {
+        const Tile8 tc = tile_at(p, tile, kTileM, NB);
+        Run8 run = blocks_of(p, tc.g, slice);
+        const int rows = (int)min((long long)kRows, p.m[tc.g] - tc.m0 - (int)rank * kRows), cols = (int)min((long long)NB, p.n[tc.g] - tc.n0);
+        const long long arow = p.row_off[tc.g] + tc.m0 + (int)rank * kRows, bcol = p.col_off[tc.g] + tc.n0;
+        for (int c = 0; c < run.count; ++c) {
+          ok = mbar_wait_warp(smem_addr(&bar_sc_empty[ss]), round ^ 1, abort_flag);
+          if (!ok) break;
+          const unsigned to = smem_addr(scales + ss * C::kScales);
+          const long long pitch = p.kblocks[run.s];
+          const float *sa = p.sa[run.s] + run.kb, *sb = p.sb[run.s] + run.kb;
+          auto copy = [&](unsigned dst, const float* base, const float* from, bool in) {
+            in = in && SBP_GUARD(from, 4);
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(in ? from : base), "r"(in ? 4u : 0u) : "memory");
+          };
+#pragma unroll
+          for (int i = 0; i < kRows; i += 64) {
+            const long long r = arow + t + i;
+            copy(to + (t + i) * 4, sa, sa + (p.a_tiles ? r >> 7 : r) * pitch, t + i < rows);
+          }
+          if (p.per_column) {
+#pragma unroll
+            for (int i = 0; i < NB; i += 64) {
+              const long long r = bcol + t + i;
+              if (t + i < NB) copy(to + (kRows + t + i) * 4, sb, sb + (p.b_tiles ? r >> 7 : r) * pitch, t + i < cols);
+            }
+          } else if (t < (NB + 127) / 128) {
+            copy(to + (kRows + t) * 4, sb, sb + ((bcol >> 7) + t) * pitch, t * 128 < cols);
+          }
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&bar_sc_full[ss])) : "memory");
+          if (++ss == kScaleSlots) { ss = 0; round ^= 1; }
+          next_block(p, run);
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (warp >= 12 && !TMA) {
+      // ------------------------------------------------ operands, by plain loads: eight threads a row
+      const int t = tid - 384, chunk = t & 7;
+      int slot = 0;
+      unsigned round = 0;
+      bool ok = true;
+      for (int tile = first; tile < p.total_tiles && ok; tile += stride) {
+        const Tile8 tc = tile_at(p, tile, kTileM, NB);
+        Run8 run = blocks_of(p, tc.g, slice);
+        const int rows = (int)min((long long)kRows, p.m[tc.g] - tc.m0), cols = (int)min((long long)NB, p.n[tc.g] - tc.n0);
+        for (int c = 0; c < run.count; ++c) {
+          ok = mbar_wait_warp(smem_addr(&bar_empty[slot]), round ^ 1, abort_flag);
+          if (!ok) break;
+          unsigned char* sa = smem + slot * C::kSlot;
+          const long long k = (long long)run.kb * 128 + chunk * 16, len = p.kseg[run.s];
+          const unsigned char* A = p.a[run.s] + (p.row_off[tc.g] + tc.m0) * p.lda[run.s];
+          const unsigned char* B = p.b[run.s] + (p.col_off[tc.g] + tc.n0) * p.ldb[run.s];
+          for (int r = t >> 3; r < kRows; r += 16)
+            *reinterpret_cast<uint4*>(sa + r * 128 + ((chunk ^ (r & 7)) << 4)) = r < rows && k < len ? row_bytes(A + r * p.lda[run.s], k, len) : make_uint4(0u, 0u, 0u, 0u);
+          for (int r = t >> 3; r < NB; r += 16)
+            *reinterpret_cast<uint4*>(sa + kRows * 128 + r * 128 + ((chunk ^ (r & 7)) << 4)) =
+                r < cols && k < len ? row_bytes(B + r * p.ldb[run.s], k, len) : make_uint4(0u, 0u, 0u, 0u);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_addr(&bar_full[slot]));
+          if (++slot == C::kSlots) { slot = 0; round ^= 1; }
+          next_block(p, run);
+        }
+      }
+    }
+    __syncwarp();
+  }
+
+  if constexpr (!PAIR) {
+    if (splits > 1) {
+      // every CTA adds up its share of the tile, slice by slice, and stores it
+      cluster_sync_all();
+      if (!*abort_flag && warp < kAccWarps) {
+        const Tile8 tc = tile_at(p, first, kTileM, NB);
+        const long long M = p.m[tc.g], N = p.n[tc.g], ldy = p.ldy[tc.g];
+        const int n_out = (tc.g == 0 ? p.n_rep : 0) + 1;
+        const int lo = kRows * NB * slice / splits, hi = kRows * NB * (slice + 1) / splits;
+        for (int e = lo + tid; e < hi; e += kAccWarps * 32) {
+          const int r = p.swap ? e & (kRows - 1) : e / NB, c = p.swap ? e / kRows : e % NB;
+          const unsigned at = smem_addr(smem) + (unsigned)(r * (NB + 1) + c) * 4;
+          float v = 0.f;
+          for (int s = 0; s < splits; ++s) {
+            float x;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(map_to_cta(at, s)) : "memory");
+            v = s == 0 ? x : v + x;
+          }
+          const long long m = tc.m0 + r, n = tc.n0 + c;
+          if (m < M && n < N)
+            for (int o = 0; o < n_out; ++o) store_one(p, o == 0 ? p.y[tc.g] : p.y_rep[o - 1], p.swap ? n * ldy + m : m * ldy + n, v);
+        }
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncwarp();
+  if (PAIR || splits > 1) cluster_sync_all();      // the partner may still signal this CTA's barriers or read its tile
+  else __syncthreads();
+  if (warp == 9) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+  }
+}
+
+// Launch of one form, or (p null) the clusters of it that the current device holds at once.
+template <bool PAIR, int NB, bool TMA>
+sbp_status launch8_form(const Params8* p, int cluster, int ctas, cudaStream_t st, int* capacity) {
+  using C = Shape8<PAIR, NB, TMA>;
+  static std::atomic<unsigned long long> opted{0};      // one bit per device
+  int dev = 0;
+  SBP_CUDA_TRY(cudaGetDevice(&dev));
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (dev >= 64 || !(opted.load(std::memory_order_relaxed) & bit)) {
+    SBP_CUDA_TRY(cudaFuncSetAttribute(matmul8_kernel<PAIR, NB, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    if constexpr (PAIR) {      // the accumulators' registers come out of what the block was launched with
+      cudaFuncAttributes attr;
+      SBP_CUDA_TRY(cudaFuncGetAttributes(&attr, matmul8_kernel<PAIR, NB, TMA>));
+      if (attr.numRegs < 168) return fail(SBP_ERR_UNSUPPORTED, "the 8-bit matmul kernel was built with %d registers a thread", attr.numRegs);
+    }
+    if (dev < 64) opted.fetch_or(bit, std::memory_order_relaxed);
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p ? 2 : 1;
+  if (!p) {
+    cfg.gridDim = dim3((unsigned)(device_sms() / cluster * cluster));
+    SBP_CUDA_TRY(cudaOccupancyMaxActiveClusters(capacity, matmul8_kernel<PAIR, NB, TMA>, &cfg));
+    return SBP_OK;
+  }
+  SBP_BOUNDS_UPLOAD(st);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, matmul8_kernel<PAIR, NB, TMA>, *p);
+  if (e != cudaSuccess) return cuda_fail(e, "8-bit matmul launch");
+  count_launch();
+  return SBP_OK;
+}
+
+// CTA pairs that the device holds at once, asked once a device.
+int pair_capacity() {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return device_sms() / 2;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (launch8_form<true, 256, true>(nullptr, 2, 0, nullptr, &n) != SBP_OK || n < 1) {
+      cudaGetLastError();
+      n = device_sms() / 2;
+    }
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+struct Form8 {
+  bool pair, swap;
+  int nb, splits;
+};
+
+long long tiles_of(const MatmulPlan& plan, int tm, int tn, bool swap) {
+  long long t = 0;
+  for (int g = 0; g < plan.ngroups; ++g)
+    if (plan.m[g] > 0 && plan.n[g] > 0)
+      t += ((swap ? plan.n[g] : plan.m[g]) + tm - 1) / tm * (((swap ? plan.m[g] : plan.n[g]) + tn - 1) / tn);
+  return t;
+}
+
+Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma) {
+  long long m = 0, n = 0;
+  for (int g = 0; g < plan.ngroups; ++g) {
+    m = std::max(m, plan.m[g]);
+    n = std::max(n, plan.n[g]);
+  }
+  const int sms = device_sms();
+  if (tma && m > 64 && n > 64 && tiles_of(plan, 256, 256, false) * 4 >= pair_capacity() * 3) return {true, false, 256, 1};
+  Form8 f{false, m < n && m <= 64, 128, 1};
+  const long long few = std::min(m, n);
+  if (few <= 64) f.nb = few <= 16 ? 16 : few <= 32 ? 32 : 64;
+  const long long tiles = tiles_of(plan, 128, f.nb, f.swap);
+  while (f.splits < 8 && tiles * f.splits * 2 <= sms && blocks >= f.splits * 4) f.splits *= 2;
+  return f;
+}
+
+sbp_status launch8(const Params8& p, Form8 f, bool tma, cudaStream_t st) {
+  const int ctas = f.pair ? 2 * std::min(p.total_tiles, pair_capacity()) : p.total_tiles * f.splits;
+  const int cluster = f.pair ? 2 : f.splits;
+  if (f.pair) return launch8_form<true, 256, true>(&p, cluster, ctas, st, nullptr);
+  switch (f.nb + (tma ? 0 : 1)) {
+    case 16: return launch8_form<false, 16, true>(&p, cluster, ctas, st, nullptr);
+    case 17: return launch8_form<false, 16, false>(&p, cluster, ctas, st, nullptr);
+    case 32: return launch8_form<false, 32, true>(&p, cluster, ctas, st, nullptr);
+    case 33: return launch8_form<false, 32, false>(&p, cluster, ctas, st, nullptr);
+    case 64: return launch8_form<false, 64, true>(&p, cluster, ctas, st, nullptr);
+    case 65: return launch8_form<false, 64, false>(&p, cluster, ctas, st, nullptr);
+    case 128: return launch8_form<false, 128, true>(&p, cluster, ctas, st, nullptr);
+    default: return launch8_form<false, 128, false>(&p, cluster, ctas, st, nullptr);
+  }
+}
+
+sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const sbp_tensor* w_scales, bool x_tiles, bool w_tiles,
+                       cudaStream_t st) {
+  bool tma = true;
+  long long blocks = 0;
+  int kblocks[SBP_MAX_K];
+  for (int s = 0; s < plan.nseg; ++s) {
+    if (plan.kseg[s] > (1LL << 31) - 256) return fail(SBP_ERR_UNSUPPORTED, "contraction too long for one launch");
+    kblocks[s] = (int)blocks8(plan.kseg[s]);
+    if (!plan.chain && s >= plan.ngroups) continue;
+    blocks = plan.chain ? blocks + kblocks[s] : std::max<long long>(blocks, kblocks[s]);
+    if (plan.kseg[s] == 0) continue;
+    for (const void* base : {plan.a[s], plan.b[s]}) tma = tma && reinterpret_cast<uintptr_t>(base) % 16 == 0;
+    tma = tma && plan.lda[s] % 16 == 0 && plan.ldb[s] % 16 == 0;
+  }
+  if (blocks > 0x7fffffffLL) return fail(SBP_ERR_UNSUPPORTED, "contraction too long for one launch");
+  const Form8 f = choose8(plan, blocks, tma);
+  Params8 p{};
+  p.splits = f.splits;
+  p.swap = f.swap;
+  p.out_f32 = plan.out_dtype == SBP_F32;
+  p.chain = plan.chain;
+  p.nseg = plan.nseg;
+  p.ngroups = plan.ngroups;
+  p.n_rep = plan.n_rep;
+  for (int r = 0; r < plan.n_rep; ++r) p.y_rep[r] = plan.y_rep[r];
+  p.a_tiles = f.swap ? w_tiles : x_tiles;
+  p.b_tiles = f.swap ? x_tiles : w_tiles;
+  const int tm = f.pair ? 256 : 128;
+  long long rows_all = 0, cols_all = 0, tiles = 0;
+  bool whole_blocks = p.b_tiles != 0;              // of columns: 128 of a tile share a scale
+  for (int g = 0; g < plan.ngroups; ++g) {
+    const bool sw = f.swap;
+    p.m[g] = sw ? plan.n[g] : plan.m[g];
+    p.n[g] = sw ? plan.m[g] : plan.n[g];
+    p.row_off[g] = sw ? plan.col_off[g] : plan.row_off[g];
+    p.col_off[g] = sw ? plan.row_off[g] : plan.col_off[g];
+    p.ldy[g] = plan.ldy[g];
+    p.y[g] = plan.y[g];
+    if (p.row_off[g] + p.m[g] > 0x7ffffe00LL || p.col_off[g] + p.n[g] > 0x7ffffe00LL) return fail(SBP_ERR_UNSUPPORTED, "matrix too large for one launch");
+    if (p.col_off[g] % 128 != 0) whole_blocks = false;
+    rows_all = std::max(rows_all, p.row_off[g] + p.m[g]);
+    cols_all = std::max(cols_all, p.col_off[g] + p.n[g]);
+    p.tile_begin[g] = (int)tiles;
+    p.tiles_m[g] = (int)std::max(1LL, (p.m[g] + tm - 1) / tm);
+    p.tiles_n[g] = (int)std::max(1LL, (p.n[g] + f.nb - 1) / f.nb);
+    if (p.m[g] > 0 && p.n[g] > 0) tiles += (long long)p.tiles_m[g] * p.tiles_n[g];
+    if (tiles > 0x07ffffffLL) return fail(SBP_ERR_UNSUPPORTED, "matrix too large for one launch");
+  }
+  for (int g = plan.ngroups; g <= SBP_MAX_K; ++g) p.tile_begin[g] = (int)tiles;
+  p.total_tiles = (int)tiles;
+  p.per_column = !whole_blocks;
+  if (tiles == 0) return SBP_OK;
+  for (int s = 0; s < plan.nseg; ++s) {
+    p.kblocks[s] = kblocks[s];
+    if (!plan.chain && s >= plan.ngroups) continue;
+    const sbp_tensor *as = f.swap ? w_scales : x_scales, *bs = f.swap ? x_scales : w_scales;
+    p.a[s] = static_cast<const unsigned char*>(f.swap ? plan.b[s] : plan.a[s]);
+    p.b[s] = static_cast<const unsigned char*>(f.swap ? plan.a[s] : plan.b[s]);
+    p.lda[s] = f.swap ? plan.ldb[s] : plan.lda[s];
+    p.ldb[s] = f.swap ? plan.lda[s] : plan.ldb[s];
+    p.kseg[s] = plan.kseg[s];
+    p.sa[s] = static_cast<const float*>(as->local[s]);
+    p.sb[s] = static_cast<const float*>(bs->local[s]);
+    const long long rows = plan.chain ? rows_all : p.m[s], cols = plan.chain ? cols_all : p.n[s];
+    if (!tma || kblocks[s] == 0 || rows == 0 || cols == 0) continue;
+    if (!tensor_map8(&p.map_a[s], p.a[s], rows, p.kseg[s], p.lda[s], kRows) ||
+        !tensor_map8(&p.map_b[s], p.b[s], cols, p.kseg[s], p.ldb[s], f.pair ? 128 : f.nb))
+      return fail(SBP_ERR_CUDA, "cuTensorMapEncodeTiled failed for an operand of shard %d", s);
+  }
+  return launch8(p, f, tma, st);
+}
+
+}  // namespace
+
+sbp_status read_and_clear_matmul8_timeout(bool* timed_out) { return read_and_clear_timeout_flag(timed_out); }
+
+}  // namespace sbp
+
+using namespace sbp;
+
+extern "C" {
+
+sbp_status sbp_matmul8(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales, sbp_tensor* y,
+                       void* cuda_stream) {
+  SBP_RANGE("sbp_matmul8");
+  MatmulPlan plan;
+  sbp_status st = build_matmul_plan(x, w, y, SBP_TRANS_W, true, true, &plan);
+  if (st != SBP_OK) return st;
+  bool x_tiles = false, w_tiles = false;
+  if ((st = check_blocks8(x, x_scales, "x", -1, true, &x_tiles)) != SBP_OK) return st;
+  if ((st = check_blocks8(w, w_scales, "w", -1, true, &w_tiles)) != SBP_OK) return st;
+  SBP_BOUNDS_RESET();
+  SBP_BOUNDS_TENSOR(x);
+  SBP_BOUNDS_TENSOR(x_scales);
+  SBP_BOUNDS_TENSOR(w);
+  SBP_BOUNDS_TENSOR(w_scales);
+  SBP_BOUNDS_TENSOR(y);
+  return run_matmul8(plan, x_scales, w_scales, x_tiles, w_tiles, static_cast<cudaStream_t>(cuda_stream));
+}
+
+}  // extern "C"

@@ -1513,6 +1513,7 @@ constexpr int kMapCacheSets = 2048, kMapCacheWays = 2;
 static MapSlot g_map_cache[kMapCacheSets][kMapCacheWays];
 static unsigned char g_map_victim[kMapCacheSets];
 static unsigned long long g_map_hits = 0, g_map_encodes = 0;
+static std::mutex g_map_mutex;      // the cache's, and that of the parameter block filled from it
 
 static unsigned map_slot_of(const MapKey& k) {
   unsigned long long h = reinterpret_cast<uintptr_t>(k.base) >> 4;
@@ -1591,7 +1592,7 @@ static bool make_map(CUtensorMap* map, const void* base, int esz, long long rows
   cuuint64_t strides[1] = {(cuuint64_t)ld * esz};
   cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
-  CUtensorMapDataType dt = esz == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  CUtensorMapDataType dt = esz == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : esz == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
   if (fn(map, dt, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return false;
@@ -1600,6 +1601,12 @@ static bool make_map(CUtensorMap* map, const void* base, int esz, long long rows
   slot.key = key;
   slot.used = true;
   return true;
+}
+
+// Maps of 8-bit operands, for the kernel that multiplies them (matmul8.cu): boxes of box_rows rows of 128 bytes.
+bool tensor_map8(CUtensorMap* map, const void* base, long long rows, long long cols, long long ld, int box_rows) {
+  std::lock_guard<std::mutex> lock(g_map_mutex);
+  return make_map(map, base, 1, rows, cols, ld, box_rows, 128);
 }
 
 static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -2162,8 +2169,7 @@ static sbp_status run_matmul_tc(const MatmulPlan& plan, const XentFusion* xf, vo
   }
 
   static TcParams p;          // large; filled under a lock and copied by value at launch
-  static std::mutex mu;
-  std::lock_guard<std::mutex> lock(mu);
+  std::lock_guard<std::mutex> lock(g_map_mutex);
 
   if (xf && forced_form() == 0 && pair_cap() == 0) {
     const sbp_status ns = launch_narrow(plan, *xf, st, taken);

@@ -2,6 +2,7 @@
 #include <atomic>
 #include <cstring>
 
+#include "blocks8.h"
 #include "bounds_check.h"
 #include "sbp_internal.h"
 
@@ -89,11 +90,12 @@ sbp_status cuda_fail(cudaError_t e, const char* what) {
   return fail(SBP_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-static sbp_status check_common(const sbp_tensor* t, const char* name, bool need_ptrs, bool allow_2d) {
+static sbp_status check_common(const sbp_tensor* t, const char* name, bool need_ptrs, bool allow_2d, bool allow_8bit = false) {
   if (!t) return fail(SBP_ERR_INVALID_ARG, "%s: null descriptor", name);
   if (t->ndim < 1 || t->ndim > SBP_MAX_DIMS)
     return fail(SBP_ERR_INVALID_ARG, "%s: ndim %d outside [1,%d]", name, t->ndim, SBP_MAX_DIMS);
   if (elem_size(t->dtype) == 0) return fail(SBP_ERR_DTYPE, "%s: unknown dtype %d", name, t->dtype);
+  if (t->dtype == SBP_E4M3 && !allow_8bit) return fail(SBP_ERR_DTYPE, "%s: E4M3 values are taken only by the entry points on 8-bit blocks", name);
   for (int d = 0; d < t->ndim; ++d)
     if (t->shape[d] < 0) return fail(SBP_ERR_SHAPE, "%s: negative extent on axis %d", name, d);
   if (t->pdims < 1 || t->pdims > SBP_MAX_PDIMS)
@@ -137,6 +139,43 @@ sbp_status check_tensor(const sbp_tensor* t, const char* name, bool need_ptrs) {
 
 sbp_status check_tensor_nd(const sbp_tensor* t, const char* name, bool need_ptrs) {
   return check_common(t, name, need_ptrs, true);
+}
+
+sbp_status check_tensor8(const sbp_tensor* t, const char* name, bool need_ptrs) {
+  return check_common(t, name, need_ptrs, false, true);
+}
+
+// Extent of the scales along an axis of the values: the blocks of every shard where the axis is split.
+static int64_t scales_extent(const sbp_tensor* values, int axis) {
+  const sbp_sig s = values->sbp[0];
+  if (s.kind != SBP_SPLIT || s.axis != axis) return blocks8(values->shape[axis]);
+  int64_t n = 0;
+  for (int r = 0; r < placement_k(values); ++r) {
+    int64_t start, len;
+    split_range(values->shape[axis], placement_k(values), r, &start, &len);
+    n += blocks8(len);
+  }
+  return n;
+}
+
+sbp_status check_blocks8(const sbp_tensor* values, const sbp_tensor* scales, const char* name, int tiles, bool need_ptrs, bool* is_tiles) {
+  sbp_status st = check_tensor8(values, name, need_ptrs);
+  if (st != SBP_OK) return st;
+  if (values->dtype != SBP_E4M3) return fail(SBP_ERR_DTYPE, "%s must be E4M3", name);
+  if ((st = check_tensor(scales, "scales", need_ptrs)) != SBP_OK) return st;
+  if (scales->dtype != SBP_F32) return fail(SBP_ERR_DTYPE, "the scales of %s must be F32", name);
+  if ((st = refuse_ld(scales, "scales", "8-bit blocks")) != SBP_OK) return st;
+  if (placement_k(values) != placement_k(scales)) return fail(SBP_ERR_INVALID_ARG, "%s and its scales differ in k", name);
+  if (!same_sig(values->sbp[0], scales->sbp[0])) return fail(SBP_ERR_SIGNATURE, "%s and its scales differ in signature", name);
+  if (scales->ndim != values->ndim) return fail(SBP_ERR_SHAPE, "%s and its scales differ in rank", name);
+  const int last = values->ndim - 1;
+  bool as_rows = true;
+  for (int d = 0; d < last; ++d) as_rows = as_rows && scales->shape[d] == values->shape[d];
+  const bool as_tiles = values->ndim == 2 && scales->shape[0] == scales_extent(values, 0);
+  if (scales->shape[last] != scales_extent(values, last) || (tiles == 1 ? !as_tiles : tiles == 0 ? !as_rows : !as_rows && !as_tiles))
+    return fail(SBP_ERR_SHAPE, "the scales of %s do not have the extents that its blocks need", name);
+  if (is_tiles) *is_tiles = !as_rows;
+  return SBP_OK;
 }
 
 void local_shape_nd(const sbp_tensor* t, int r, int64_t out[SBP_MAX_DIMS]) {
@@ -200,6 +239,7 @@ __global__ void bounds_selftest_kernel(unsigned char* buf, size_t bytes) {
 sbp_status read_and_clear_bulk_timeout(bool* timed_out);
 sbp_status read_and_clear_tc_timeout(bool* timed_out);
 sbp_status read_and_clear_f32_tc_timeout(bool* timed_out);
+sbp_status read_and_clear_matmul8_timeout(bool* timed_out);
 sbp_status launch_expire_wait(unsigned long long limit_ns, cudaStream_t st);
 
 }  // namespace sbp
@@ -238,12 +278,14 @@ int32_t sbp_debug_bounds_enabled(void) {
 uint64_t sbp_launch_count(void) { return g_launches.load(std::memory_order_relaxed); }
 
 sbp_status sbp_check_device_errors(void) {
-  bool bulk = false, tc = false, f32 = false;
+  bool bulk = false, tc = false, f32 = false, eight = false;
   sbp_status st = read_and_clear_bulk_timeout(&bulk);
   if (st != SBP_OK) return st;
   st = read_and_clear_tc_timeout(&tc);
   if (st != SBP_OK) return st;
   st = read_and_clear_f32_tc_timeout(&f32);
+  if (st != SBP_OK) return st;
+  st = read_and_clear_matmul8_timeout(&eight);
   if (st != SBP_OK) return st;
 #ifdef SBP_DEBUG_BOUNDS
   if (cudaDeviceSynchronize() != cudaSuccess) return fail(SBP_ERR_CUDA, "device synchronisation failed");
@@ -254,7 +296,7 @@ sbp_status sbp_check_device_errors(void) {
   }
 #endif
   if (bulk) return fail(SBP_ERR_TIMEOUT, "a bulk-copy boxing kernel gave up waiting for its loads");
-  if (tc || f32) return fail(SBP_ERR_TIMEOUT, "the tensor-core matmul kernel gave up waiting on one of its barriers");
+  if (tc || f32 || eight) return fail(SBP_ERR_TIMEOUT, "the tensor-core matmul kernel gave up waiting on one of its barriers");
   return SBP_OK;
 }
 
@@ -282,12 +324,24 @@ sbp_status sbp_selftest_wait_timeout(uint32_t limit_ms, void* cuda_stream) {
 }
 
 sbp_status sbp_local_shape(const sbp_tensor* t, int32_t r, int64_t out_shape[SBP_MAX_DIMS]) {
-  sbp_status st = check_tensor_nd(t, "t", false);
+  sbp_status st = check_common(t, "t", false, true, true);
   if (st != SBP_OK) return st;
   if (!out_shape) return fail(SBP_ERR_INVALID_ARG, "out_shape is null");
   int k = placement_k(t);
   if (r < 0 || r >= k) return fail(SBP_ERR_INVALID_ARG, "shard %d outside [0,%d)", r, k);
   local_shape_nd(t, r, out_shape);
+  return SBP_OK;
+}
+
+sbp_status sbp_scales_shape(const sbp_tensor* values, uint32_t flags, int64_t out_shape[SBP_MAX_DIMS]) {
+  if (flags & ~SBP_QUANT_TILES) return fail(SBP_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  sbp_status st = check_tensor8(values, "values", false);
+  if (st != SBP_OK) return st;
+  if (!out_shape) return fail(SBP_ERR_INVALID_ARG, "out_shape is null");
+  if ((flags & SBP_QUANT_TILES) && values->ndim != 2) return fail(SBP_ERR_SHAPE, "tiles need a 2-D tensor");
+  for (int d = 0; d < SBP_MAX_DIMS; ++d) out_shape[d] = d < values->ndim ? values->shape[d] : 1;
+  out_shape[values->ndim - 1] = scales_extent(values, values->ndim - 1);
+  if (flags & SBP_QUANT_TILES) out_shape[0] = scales_extent(values, 0);
   return SBP_OK;
 }
 

@@ -31,6 +31,7 @@ inline int elem_size(int32_t dtype) {
     case SBP_F32: return 4;
     case SBP_BF16: return 2;
     case SBP_I64: return 8;
+    case SBP_E4M3: return 1;
     default: return 0;
   }
 }
@@ -60,7 +61,7 @@ void local_shape_nd(const sbp_tensor* t, int r, int64_t out[SBP_MAX_DIMS]);
 // Same checks as check_tensor but also accepts a two-axis placement (Section 3.3).
 sbp_status check_tensor_nd(const sbp_tensor* t, const char* name, bool need_ptrs);
 
-// Full validation of a descriptor (rank, dtype, placement, signature, pointers).
+// Full validation of a descriptor (rank, dtype, placement, signature, pointers).  SBP_E4M3 is refused (check_tensor8 in blocks8.h takes it).
 // need_ptrs: every local[r], r < k, must be non-null and aligned to the element size.
 sbp_status check_tensor(const sbp_tensor* t, const char* name, bool need_ptrs);
 
