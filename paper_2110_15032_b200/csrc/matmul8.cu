@@ -6,11 +6,11 @@
 // the next block's products go to another part of tensor memory.  So any fp32 scale is taken, and what the tensor cores add up
 // unscaled is never more than 128 products.
 //
-//   warps 0-7    the accumulators: 32 rows x half of the tile's columns each, a row a thread
-//   warp 8       operands by bulk tensor copies (TMA form)
-//   warp 9       one elected lane issues the MMAs
-//   warps 10-11  the scales of a block into a ring of their own, asynchronously
-//   warps 12-15  operands by plain loads, where base or pitch is not a multiple of 16 bytes (the other form)
+//   8 warps (a pair's CTAs: 16)  the accumulators: 32 rows x 64 or fewer of the tile's columns each, a row a thread
+//   1 warp    operands by bulk tensor copies (TMA form)
+//   1 warp    one elected lane issues the MMAs
+//   2 warps   the scales of a block into a ring of their own, asynchronously
+//   4 warps   operands by plain loads, where base or pitch is not a multiple of 16 bytes (the other form)
 //
 // Forms: a CTA pair with 256 x 256 tiles, persistent; single CTAs with 128 x NB tiles, cut along the contraction over a cluster where
 // there are few of them.  Few rows (columns): the 128 rows of the tile are the other operand's.
@@ -32,18 +32,19 @@ namespace sbp {
 sbp_status build_matmul_plan(const sbp_tensor* x, const sbp_tensor* w, const sbp_tensor* y, uint32_t flags, bool need_ptrs, bool eight,
                              MatmulPlan* plan);
 bool tensor_map8(CUtensorMap* map, const void* base, long long rows, long long cols, long long ld, int box_rows);
+bool tensor_map8_out(CUtensorMap* map, const void* base, int esz, long long rows, long long cols, long long ld);
 
 namespace {
 
 constexpr int kRows = 128;                   // rows of the A operand a CTA holds
 constexpr int kRing = 168 * 1024;
-constexpr int kScaleSlots = 8;
-constexpr int kSlab = 32 * 128;              // staging of an accumulating warp: 32 rows of 128 bytes
-constexpr int kAccWarps = 8;
+constexpr int kScaleSlots = 3, kGroup = 4;   // slots of the scales' ring, blocks whose scales share one
+constexpr int kLoad8 = 32;                   // accumulator columns loaded at a time
 constexpr int kPanel = 8;                    // row tiles walked together
 
 struct Params8 {
   CUtensorMap map_a[SBP_MAX_K], map_b[SBP_MAX_K];
+  CUtensorMap map_y[SBP_MAX_K], map_rep[SBP_MAX_K];      // where y_tma is set: the result and its replicas
   // as stored, for the loading form: bases, pitches and K of every segment
   const unsigned char* a[SBP_MAX_K];
   const unsigned char* b[SBP_MAX_K];
@@ -58,11 +59,39 @@ struct Params8 {
   int n_rep, ngroups, nseg, chain, total_tiles;
   int a_tiles, b_tiles;                      // the scales are one for 128 rows (columns)
   int per_column;                            // a scale a column, else one for 128 columns of a tile
+  int y_tma;                                 // the copy engine can address the result
   int out_f32, swap;                         // swap: rows of the tile are columns of the result
   int splits;                                // CTAs of a cluster that share a tile's contraction
 };
 
 constexpr unsigned idesc8(int rows, int cols) { return (1u << 4) | ((unsigned)(cols >> 3) << 17) | ((unsigned)(rows >> 4) << 24); }
+
+// A bounded wait of a converged warp.  Without a hint how long to sleep: the wait for an accumulator is on the chain from one block's
+// products to those after the next.
+__device__ __forceinline__ bool wait_long(unsigned bar, unsigned parity, volatile int* abort_flag) {
+  const unsigned long long t0 = now_ns();
+  for (;;) {
+    for (int i = 0; i < 64; ++i) {
+      unsigned done;
+      asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                   : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+      if (__all_sync(0xffffffffu, done)) return true;
+    }
+    if (__any_sync(0xffffffffu, *abort_flag)) return false;
+    if (__any_sync(0xffffffffu, now_ns() - t0 > kWaitLimitNs)) {
+      *abort_flag = 1;
+      atomicExch(&g_tc_timeout_flag, 1);
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ bool wait8(unsigned bar, unsigned parity, volatile int* abort_flag) {
+  unsigned done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  if (__all_sync(0xffffffffu, done)) return true;
+  return wait_long(bar, parity, abort_flag);
+}
 
 template <bool PAIR>
 __device__ __forceinline__ void umma8(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned accumulate) {
@@ -82,26 +111,26 @@ __device__ __forceinline__ void tma_load_cta(unsigned dst, const CUtensorMap* ma
                : "memory");
 }
 
-// N accumulator columns of this warp's 32 rows, in pairs
+// N accumulator columns of this warp's 32 rows
 template <int N>
-__device__ __forceinline__ void tmem_pairs(unsigned taddr, unsigned long long* v) {
-  float f[N];
-  if constexpr (N == 32) tmem_ld32(taddr, f);
-  else {
-#pragma unroll
-    for (int i = 0; i < N; i += 8) tmem_ld8(taddr + i, f + i);
+__device__ __forceinline__ void tmem_columns(unsigned taddr, float (&v)[N]) {
+  if constexpr (N == 32) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+                 : "r"(taddr)
+                 : "memory");
+  } else if constexpr (N == 16) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                 : "r"(taddr)
+                 : "memory");
+  } else {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                 : "r"(taddr)
+                 : "memory");
   }
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) asm volatile("mov.b64 %0, {%1, %2};" : "=l"(v[i]) : "f"(f[2 * i]), "f"(f[2 * i + 1]));
 }
-__device__ __forceinline__ unsigned long long two8(float x, float y) {
-  unsigned long long v;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
-  return v;
-}
-__device__ __forceinline__ float lo8(unsigned long long v) { return __uint_as_float((unsigned)v); }
-__device__ __forceinline__ float hi8(unsigned long long v) { return __uint_as_float((unsigned)(v >> 32)); }
 
 template <bool PAIR, int NB, bool TMA>
 struct Shape8 {
@@ -109,8 +138,11 @@ struct Shape8 {
   static constexpr int kSlot = (kRows + kColsCta) * 128;
   static constexpr int kSlots = kRing / kSlot;                   // 5 (256 and 128 columns), 7, 8, 9
   static constexpr int kAccs = NB == 256 ? 2 : 4, kAccCols = NB == 256 ? 256 : 128;
-  static constexpr int kScales = kRows + NB;                     // floats of a block
-  static constexpr int kThreads = TMA ? 384 : 512;
+  static constexpr int kScales = kGroup * (kRows + NB);          // floats of a slot: [row][block], [block][column]
+  static constexpr int kAccWarps = 8;
+  static constexpr int kCols = NB / (kAccWarps / 4);             // columns of an accumulating warp
+  static constexpr int kSlab = 32 * 128;                         // its staging: 32 rows of 128 bytes
+  static constexpr int kThreads = (kAccWarps + (TMA ? 4 : 8)) * 32;
   static constexpr int kSmem = kSlots * kSlot + kAccWarps * kSlab + kScaleSlots * kScales * 4 + 1024;
 };
 
@@ -179,7 +211,7 @@ __device__ __forceinline__ void store_one(const Params8& p, void* y, long long a
 template <bool PAIR, int NB, bool TMA>
 __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_kernel(const __grid_constant__ Params8 p) {
   using C = Shape8<PAIR, NB, TMA>;
-  constexpr int kHalf = NB / 2;                    // columns of an accumulating warp
+  constexpr int kCols = C::kCols, kAccWarps = C::kAccWarps, kRole = kAccWarps;      // the first warp behind the accumulators
   constexpr int kTileM = PAIR ? 256 : 128;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) unsigned long long bar_full[C::kSlots], bar_empty[C::kSlots], bar_acc_full[C::kAccs], bar_acc_empty[C::kAccs],
@@ -189,7 +221,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
   volatile int* abort_flag = &abort_flag_s;
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   unsigned char* staging = smem + C::kSlots * C::kSlot;
-  float* scales = reinterpret_cast<float*>(staging + kAccWarps * kSlab);
+  float* scales = reinterpret_cast<float*>(staging + kAccWarps * C::kSlab);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const unsigned rank = PAIR ? cluster_ctarank() : 0u;
 
@@ -210,7 +242,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 9) {
+  if (warp == kRole + 1) {
     if constexpr (PAIR) {
       asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_slot)), "r"(512) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -234,114 +266,135 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
   if (warp < kAccWarps) {
     // ------------------------------------------------ accumulators
     if constexpr (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");      // 2 x 216 + 72 = 3 x 168
-    const int q = warp & 3, half = warp >> 2;
+    const int q = warp & 3, part = warp >> 2;       // lanes and columns
     const int row = q * 32 + lane;                 // of this CTA's 128
     const unsigned acc_empty0 = PAIR ? map_to_cta(smem_addr(&bar_acc_empty[0]), 0) : smem_addr(&bar_acc_empty[0]);
     int a = 0, ss = 0;
     unsigned a_round = 0, s_round = 0;
+    float4 rs4 = make_float4(0.f, 0.f, 0.f, 0.f);      // this row's scales of four blocks; times the columns' where those share one
     bool ok = true;
     for (int tile = first; tile < p.total_tiles && ok; tile += stride) {
       const Tile8 tc = tile_at(p, tile, kTileM, NB);
       const int count = blocks_of(p, tc.g, slice).count;
-      unsigned long long acc[NB / 4];
+      float acc[kCols];
 #pragma unroll
-      for (int i = 0; i < NB / 4; ++i) acc[i] = 0ull;
+      for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
       for (int c = 0; c < count; ++c) {
-        ok = mbar_wait_warp(smem_addr(&bar_sc_full[ss]), s_round, abort_flag);
-        if (!ok) break;
-        const float* sc = scales + ss * C::kScales;
-        const float rs = sc[row];
-        ok = mbar_wait_warp(smem_addr(&bar_acc_full[a]), a_round, abort_flag);
+        const int j = c % kGroup;
+        if (j == 0) {                              // the next blocks' scales
+          ok = wait8(smem_addr(&bar_sc_full[ss]), s_round, abort_flag);
+          if (!ok) break;
+          rs4 = *reinterpret_cast<const float4*>(scales + ss * C::kScales + row * kGroup);
+          if (!p.per_column) {
+            const float4 cs = *reinterpret_cast<const float4*>(scales + ss * C::kScales + (kRows + part * kCols / 128) * kGroup);
+            rs4 = make_float4(rs4.x * cs.x, rs4.y * cs.y, rs4.z * cs.z, rs4.w * cs.w);
+          }
+        }
+        const float rs = j == 0 ? rs4.x : j == 1 ? rs4.y : j == 2 ? rs4.z : rs4.w;
+        ok = wait8(smem_addr(&bar_acc_full[a]), a_round, abort_flag);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + half * kHalf;
-        constexpr int kStep = kHalf < 32 ? kHalf : 32;
+        const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + part * kCols;
+        constexpr int kStep = kCols < kLoad8 ? kCols : kLoad8;
+        // the last columns are in registers: the accumulator and the scales go back before they are added
+        auto hand_back = [&]() {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (PAIR) mbar_arrive_cluster(acc_empty0 + a * 8);
+            else mbar_arrive(acc_empty0 + a * 8);
+          }
+        };
         if (!p.per_column) {
-          const float s = rs * sc[kRows + (NB == 256 ? half : 0)];
-          const unsigned long long s2 = two8(s, s);
 #pragma unroll
-          for (int b = 0; b < kHalf; b += kStep) {
-            unsigned long long v[kStep / 2];
-            tmem_pairs<kStep>(at + b, v);
+          for (int b = 0; b < kCols; b += kStep) {
+            float v[kStep];
+            tmem_columns(at + b, v);
+            if (b + kStep == kCols) hand_back();
 #pragma unroll
-            for (int i = 0; i < kStep / 2; ++i) asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[b / 2 + i]) : "l"(v[i]), "l"(s2));
+            for (int i = 0; i < kStep; ++i) acc[b + i] = fmaf(v[i], rs, acc[b + i]);
           }
         } else {
-          const unsigned long long r2 = two8(rs, rs);
-          const float* cs = sc + kRows + half * kHalf;
+          const float* cs = scales + ss * C::kScales + kGroup * kRows + j * NB + part * kCols;
 #pragma unroll
-          for (int b = 0; b < kHalf; b += kStep) {
-            unsigned long long v[kStep / 2];
-            tmem_pairs<kStep>(at + b, v);
+          for (int b = 0; b < kCols; b += kStep) {
+            float v[kStep];
+            tmem_columns(at + b, v);
+            if (b + kStep == kCols) hand_back();
 #pragma unroll
-            for (int i = 0; i < kStep / 2; i += 2) {
-              const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(cs + b + 2 * i);
-              asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v[i]) : "l"(s.x));
-              asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v[i + 1]) : "l"(s.y));
-              asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[b / 2 + i]) : "l"(v[i]), "l"(r2));
-              asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[b / 2 + i + 1]) : "l"(v[i + 1]), "l"(r2));
+            for (int i = 0; i < kStep; i += 4) {
+              const float4 s = *reinterpret_cast<const float4*>(cs + b + i);
+              acc[b + i] = fmaf(v[i] * s.x, rs, acc[b + i]);
+              acc[b + i + 1] = fmaf(v[i + 1] * s.y, rs, acc[b + i + 1]);
+              acc[b + i + 2] = fmaf(v[i + 2] * s.z, rs, acc[b + i + 2]);
+              acc[b + i + 3] = fmaf(v[i + 3] * s.w, rs, acc[b + i + 3]);
             }
           }
         }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) {
-          if constexpr (PAIR) mbar_arrive_cluster(acc_empty0 + a * 8);
-          else mbar_arrive(acc_empty0 + a * 8);
-          mbar_arrive(smem_addr(&bar_sc_empty[ss]));
+        if (j == kGroup - 1 || c + 1 == count) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_addr(&bar_sc_empty[ss]));
+          if (++ss == kScaleSlots) { ss = 0; s_round ^= 1; }
         }
         if (++a == C::kAccs) { a = 0; a_round ^= 1; }
-        if (++ss == kScaleSlots) { ss = 0; s_round ^= 1; }
       }
       if (!ok) break;
       const long long M = p.m[tc.g], N = p.n[tc.g], ldy = p.ldy[tc.g];
       const int n_out = (tc.g == 0 ? p.n_rep : 0) + 1;
-      const long long row0 = tc.m0 + (int)rank * kRows, col0 = tc.n0 + half * kHalf;
+      const long long row0 = tc.m0 + (int)rank * kRows, col0 = tc.n0 + part * kCols;
       if (splits > 1) {                            // the partial tile, for the cluster to add up; the ring is done with
-        float* mine = reinterpret_cast<float*>(smem) + row * (NB + 1) + half * kHalf;
+        float* mine = reinterpret_cast<float*>(smem) + row * (NB + 1) + part * kCols;
         asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < kHalf / 2; ++i) {
-          mine[2 * i] = lo8(acc[i]);
-          mine[2 * i + 1] = hi8(acc[i]);
-        }
+        for (int i = 0; i < kCols; ++i) mine[i] = acc[i];
       } else if (p.swap) {                         // neighbouring lanes are neighbouring columns of the result
         const long long n = row0 + row;
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-          const float v = i & 1 ? hi8(acc[i / 2]) : lo8(acc[i / 2]);
+        for (int i = 0; i < kCols; ++i) {
           if (n < M && col0 + i < N)
-            for (int o = 0; o < n_out; ++o) store_one(p, o == 0 ? p.y[tc.g] : p.y_rep[o - 1], (col0 + i) * ldy + n, v);
+            for (int o = 0; o < n_out; ++o) store_one(p, o == 0 ? p.y[tc.g] : p.y_rep[o - 1], (col0 + i) * ldy + n, acc[i]);
         }
       } else {
         // through a slab of shared memory, so that a warp stores whole pieces of rows
-        unsigned char* slab = staging + warp * kSlab;
+        unsigned char* slab = staging + warp * C::kSlab;
         auto rows_out = [&](auto f32_tag) {
           constexpr bool F32 = decltype(f32_tag)::value;
-          constexpr int esz = F32 ? 4 : 2, kCols = kHalf < 128 / esz ? kHalf : 128 / esz, kChunks = kCols * esz / 16;
+          constexpr int esz = F32 ? 4 : 2, kPiece = kCols < 128 / esz ? kCols : 128 / esz, kChunks = kPiece * esz / 16;
           constexpr int kPer = 16 / esz;           // elements of a 16-byte chunk
-          bool vec = ldy * esz % 16 == 0;
-          for (int o = 0; o < n_out; ++o) vec = vec && (reinterpret_cast<unsigned long long>(o == 0 ? p.y[tc.g] : p.y_rep[o - 1]) & 15) == 0;
+          const long long m0 = row0 + q * 32;      // of the warp's 32
 #pragma unroll
-          for (int s = 0; s < kHalf / kCols; ++s) {
+          for (int s = 0; s < kCols / kPiece; ++s) {
+            const long long n0 = col0 + s * kPiece;
+            if (m0 >= M || n0 >= N) break;         // the same for the whole warp
+            // the store before has been read out of the slab
+            if (p.y_tma && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             __syncwarp();
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
-              const unsigned long long* f = acc + (s * kCols + c * kPer) / 2;
+              const float* f = acc + s * kPiece + c * kPer;
               uint4 o;
-              if constexpr (F32) o = make_uint4((unsigned)f[0], (unsigned)(f[0] >> 32), (unsigned)f[1], (unsigned)(f[1] >> 32));
-              else o = make_uint4(bf16_two(lo8(f[0]), hi8(f[0])), bf16_two(lo8(f[1]), hi8(f[1])), bf16_two(lo8(f[2]), hi8(f[2])), bf16_two(lo8(f[3]), hi8(f[3])));
+              if constexpr (F32) o = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+              else o = make_uint4(bf16_two(f[0], f[1]), bf16_two(f[2], f[3]), bf16_two(f[4], f[5]), bf16_two(f[6], f[7]));
               *reinterpret_cast<uint4*>(slab + lane * 128 + ((c ^ (lane & 7)) << 4)) = o;
+            }
+            if (kChunks == 8 && p.y_tma) {         // a whole slab
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) {
+                for (int o = 0; o < n_out; ++o) tma_store_2d(o == 0 ? &p.map_y[tc.g] : &p.map_rep[o - 1], (int)n0, (int)m0, smem_addr(slab));
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+              }
+              continue;
             }
             __syncwarp();
             for (int i = 0; i < kChunks; ++i) {
               const int r = i * (32 / kChunks) + lane / kChunks, c = lane % kChunks;
-              const long long m = row0 + q * 32 + r, n = col0 + s * kCols + c * kPer;
+              const long long m = m0 + r, n = n0 + c * kPer;
               if (m >= M || n >= N) continue;
               const unsigned char* from = slab + r * 128 + ((c ^ (r & 7)) << 4);
               for (int o = 0; o < n_out; ++o) {
                 unsigned char* to = static_cast<unsigned char*>(o == 0 ? p.y[tc.g] : p.y_rep[o - 1]) + (m * ldy + n) * esz;
-                if (vec && n + kPer <= N) {
+                if (p.y_tma && n + kPer <= N) {    // (that also says that whole vectors are aligned)
                   if (SBP_GUARD(to, 16)) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
                 } else {
                   for (int e = 0; e < kPer && n + e < N; ++e) {
@@ -358,9 +411,10 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
         else rows_out(std::false_type{});
       }
     }
+    if (p.y_tma && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   } else {
     if constexpr (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == 8 && TMA) {
+    if (warp == kRole && TMA) {
       // ------------------------------------------------ operands, by the copy engine
       const bool leader = elect_one();
       int slot = 0;
@@ -400,7 +454,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
           }
         }
       }
-    } else if (warp == 9) {
+    } else if (warp == kRole + 1) {
       // ------------------------------------------------ MMA issuer (PAIR: the first CTA's)
       if (rank == 0) {
         const bool leader = elect_one();
@@ -412,7 +466,8 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
           const Tile8 tc = tile_at(p, tile, kTileM, NB);
           const int count = blocks_of(p, tc.g, slice).count;
           for (int c = 0; c < count; ++c) {
-            ok = mbar_wait_warp(smem_addr(&bar_acc_empty[a]), a_round ^ 1, abort_flag) && mbar_wait_warp(smem_addr(&bar_full[slot]), round, abort_flag);
+            // (the operands are there as a rule: their wait comes first, off the chain)
+            ok = wait8(smem_addr(&bar_full[slot]), round, abort_flag) && wait8(smem_addr(&bar_acc_empty[a]), a_round ^ 1, abort_flag);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (leader) {
@@ -435,9 +490,9 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
           }
         }
       }
-    } else if (warp == 10 || warp == 11) {
+    } else if (warp == kRole + 2 || warp == kRole + 3) {
       // ------------------------------------------------ scales
-      const int t = tid - 320;
+      const int t = tid - (kRole + 2) * 32;
       int ss = 0;
       unsigned round = 0;
       bool ok = true;
@@ -446,39 +501,42 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
         Run8 run = blocks_of(p, tc.g, slice);
         const int rows = (int)min((long long)kRows, p.m[tc.g] - tc.m0 - (int)rank * kRows), cols = (int)min((long long)NB, p.n[tc.g] - tc.n0);
         const long long arow = p.row_off[tc.g] + tc.m0 + (int)rank * kRows, bcol = p.col_off[tc.g] + tc.n0;
-        for (int c = 0; c < run.count; ++c) {
+        for (int c = 0; c < run.count; c += kGroup) {
           ok = mbar_wait_warp(smem_addr(&bar_sc_empty[ss]), round ^ 1, abort_flag);
           if (!ok) break;
           const unsigned to = smem_addr(scales + ss * C::kScales);
-          const long long pitch = p.kblocks[run.s];
-          const float *sa = p.sa[run.s] + run.kb, *sb = p.sb[run.s] + run.kb;
+          const int n = min(kGroup, run.count - c);
           auto copy = [&](unsigned dst, const float* base, const float* from, bool in) {
             in = in && SBP_GUARD(from, 4);
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(in ? from : base), "r"(in ? 4u : 0u) : "memory");
           };
+          for (int j = 0; j < n; ++j) {
+            const long long pitch = p.kblocks[run.s];
+            const float *sa = p.sa[run.s] + run.kb, *sb = p.sb[run.s] + run.kb;
 #pragma unroll
-          for (int i = 0; i < kRows; i += 64) {
-            const long long r = arow + t + i;
-            copy(to + (t + i) * 4, sa, sa + (p.a_tiles ? r >> 7 : r) * pitch, t + i < rows);
-          }
-          if (p.per_column) {
-#pragma unroll
-            for (int i = 0; i < NB; i += 64) {
-              const long long r = bcol + t + i;
-              if (t + i < NB) copy(to + (kRows + t + i) * 4, sb, sb + (p.b_tiles ? r >> 7 : r) * pitch, t + i < cols);
+            for (int i = 0; i < kRows; i += 64) {
+              const long long r = arow + t + i;
+              copy(to + ((t + i) * kGroup + j) * 4, sa, sa + (p.a_tiles ? r >> 7 : r) * pitch, t + i < rows);
             }
-          } else if (t < (NB + 127) / 128) {
-            copy(to + (kRows + t) * 4, sb, sb + ((bcol >> 7) + t) * pitch, t * 128 < cols);
+            if (p.per_column) {
+#pragma unroll
+              for (int i = 0; i < NB; i += 64) {
+                const long long r = bcol + t + i;
+                if (t + i < NB) copy(to + (kGroup * kRows + j * NB + t + i) * 4, sb, sb + (p.b_tiles ? r >> 7 : r) * pitch, t + i < cols);
+              }
+            } else if (t < (NB + 127) / 128) {
+              copy(to + ((kRows + t) * kGroup + j) * 4, sb, sb + ((bcol >> 7) + t) * pitch, t * 128 < cols);
+            }
+            next_block(p, run);
           }
           asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&bar_sc_full[ss])) : "memory");
           if (++ss == kScaleSlots) { ss = 0; round ^= 1; }
-          next_block(p, run);
         }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (warp >= 12 && !TMA) {
+    } else if (warp >= kRole + 4 && !TMA) {
       // ------------------------------------------------ operands, by plain loads: eight threads a row
-      const int t = tid - 384, chunk = t & 7;
+      const int t = tid - (kRole + 4) * 32, chunk = t & 7;
       int slot = 0;
       unsigned round = 0;
       bool ok = true;
@@ -538,7 +596,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
   __syncwarp();
   if (PAIR || splits > 1) cluster_sync_all();      // the partner may still signal this CTA's barriers or read its tile
   else __syncthreads();
-  if (warp == 9) {
+  if (warp == kRole + 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
@@ -701,6 +759,17 @@ sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const
   p.total_tiles = (int)tiles;
   p.per_column = !whole_blocks;
   if (tiles == 0) return SBP_OK;
+  const int esz = p.out_f32 ? 4 : 2;
+  bool y_tma = !f.swap && f.splits == 1;
+  for (int g = 0; g < plan.ngroups; ++g)
+    if (p.m[g] > 0 && p.n[g] > 0) y_tma = y_tma && reinterpret_cast<uintptr_t>(p.y[g]) % 16 == 0 && p.ldy[g] * esz % 16 == 0;
+  for (int r = 0; r < p.n_rep; ++r) y_tma = y_tma && reinterpret_cast<uintptr_t>(p.y_rep[r]) % 16 == 0;
+  p.y_tma = y_tma;
+  for (int g = 0; y_tma && g < plan.ngroups; ++g)
+    if (p.m[g] > 0 && p.n[g] > 0 && !tensor_map8_out(&p.map_y[g], p.y[g], esz, p.m[g], p.n[g], p.ldy[g]))
+      return fail(SBP_ERR_CUDA, "cuTensorMapEncodeTiled failed for the result of group %d", g);
+  for (int r = 0; y_tma && r < p.n_rep; ++r)
+    if (!tensor_map8_out(&p.map_rep[r], p.y_rep[r], esz, p.m[0], p.n[0], p.ldy[0])) return fail(SBP_ERR_CUDA, "cuTensorMapEncodeTiled failed for a result replica");
   for (int s = 0; s < plan.nseg; ++s) {
     p.kblocks[s] = kblocks[s];
     if (!plan.chain && s >= plan.ngroups) continue;

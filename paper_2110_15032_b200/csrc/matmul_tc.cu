@@ -1608,6 +1608,11 @@ bool tensor_map8(CUtensorMap* map, const void* base, long long rows, long long c
   std::lock_guard<std::mutex> lock(g_map_mutex);
   return make_map(map, base, 1, rows, cols, ld, box_rows, 128);
 }
+// and of its result: boxes of 32 rows of 128 bytes.
+bool tensor_map8_out(CUtensorMap* map, const void* base, int esz, long long rows, long long cols, long long ld) {
+  std::lock_guard<std::mutex> lock(g_map_mutex);
+  return make_map(map, base, esz, rows, cols, ld, 32, 128 / esz);
+}
 
 static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
