@@ -53,33 +53,86 @@ __device__ __forceinline__ unsigned finite_bits(float v) {
 // v, or NaN where v is infinite (the conversion would saturate it)
 __device__ __forceinline__ float inf_to_nan(float v) { return v + (v - v); }
 
-// Eight consecutive elements to and from fp32.  VEC: all of them are there, 16-byte aligned; else the first `n` are, apart by `step`
-// elements (so that neighbouring lanes may take neighbouring ones).
-template <bool VEC>
-__device__ __forceinline__ void load8(const float* p, float* v, int n = 8, int step = 1) {
-  if constexpr (VEC) {
-    const float4 a = SBP_GUARD(p, 32) ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
-    const float4 b = SBP_GUARD(p, 32) ? *reinterpret_cast<const float4*>(p + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n && SBP_GUARD(p + e * step, 4) ? p[e * step] : 0.f;
+// Eight elements of a row as they were loaded, so that loads may be ahead of their use at no more registers than the bytes need.
+// VEC: they follow one another, all are there and the first is 16-byte aligned; else the first `n` are there, `step` elements apart (so that
+// neighbouring lanes may take neighbouring ones).
+template <typename T, bool VEC>
+struct Eight;
+template <>
+struct Eight<float, true> {
+  float4 a, b;
+  __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void load(const float* p, int, int) {
+    clear();
+    if (SBP_GUARD(p, 32)) {
+      a = __ldcs(reinterpret_cast<const float4*>(p));
+      b = __ldcs(reinterpret_cast<const float4*>(p + 4));
+    }
   }
-}
-template <bool VEC>
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* v, int n = 8, int step = 1) {
-  if constexpr (VEC) {
-    const uint4 a = SBP_GUARD(p, 16) ? *reinterpret_cast<const uint4*>(p) : make_uint4(0u, 0u, 0u, 0u);
+  __device__ __forceinline__ void get(float* v) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+};
+template <>
+struct Eight<__nv_bfloat16, true> {
+  uint4 a;
+  __device__ __forceinline__ void clear() { a = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int, int) {
+    clear();
+    if (SBP_GUARD(p, 16)) a = __ldcs(reinterpret_cast<const uint4*>(p));
+  }
+  __device__ __forceinline__ void get(float* v) const {
     const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[2 * e] = __uint_as_float(w[e] << 16);
       v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n && SBP_GUARD(p + e * step, 2) ? __bfloat162float(p[e * step]) : 0.f;
   }
+};
+template <typename T>
+struct Eight<T, false> {
+  float v_[8];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v_[e] = 0.f;
+  }
+  __device__ __forceinline__ void load(const T* p, int n, int step) {
+    if (n == 8 && SBP_GUARD(p, sizeof(T)) && SBP_GUARD(p + 7 * step, sizeof(T))) {      // (no test an element)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v_[e] = (float)p[e * step];
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v_[e] = e < n && SBP_GUARD(p + e * step, sizeof(T)) ? (float)p[e * step] : 0.f;
+  }
+  __device__ __forceinline__ void get(float* v) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = v_[e];
+  }
+};
+
+// Bits of the largest magnitude of eight numbers; infinities and NaN are larger than all numbers.
+template <typename T, bool VEC>
+__device__ __forceinline__ unsigned largest_bits(const Eight<T, VEC>& x) {
+  float v[8];
+  x.get(v);
+  unsigned m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
+  return m;
+}
+__device__ __forceinline__ unsigned largest_bits(const Eight<__nv_bfloat16, true>& x) {      // in pairs
+  constexpr unsigned kMag = 0x7fff7fffu;
+  const unsigned m = __vmaxs2(__vimax3_s16x2(x.a.x & kMag, x.a.y & kMag, x.a.z & kMag), x.a.w & kMag);
+  return max(m << 16, m & 0xffff0000u);
+}
+
+template <bool VEC, typename T>
+__device__ __forceinline__ void load8(const T* p, float* v, int n = 8, int step = 1) {
+  Eight<T, VEC> x;
+  x.load(p, n, step);
+  x.get(v);
 }
 __device__ __forceinline__ unsigned bf16_two(float lo, float hi) {
   unsigned r;
@@ -90,9 +143,12 @@ template <bool VEC>
 __device__ __forceinline__ void store8(float* p, const float* v, int n = 8, int step = 1) {
   if constexpr (VEC) {
     if (SBP_GUARD(p, 32)) {
-      *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+      __stcs(reinterpret_cast<float4*>(p + 4), make_float4(v[4], v[5], v[6], v[7]));
     }
+  } else if (n == 8 && SBP_GUARD(p, 4) && SBP_GUARD(p + 7 * step, 4)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e * step] = v[e];
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -103,7 +159,10 @@ template <bool VEC>
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* v, int n = 8, int step = 1) {
   if constexpr (VEC) {
     if (SBP_GUARD(p, 16))
-      *reinterpret_cast<uint4*>(p) = make_uint4(bf16_two(v[0], v[1]), bf16_two(v[2], v[3]), bf16_two(v[4], v[5]), bf16_two(v[6], v[7]));
+      __stcs(reinterpret_cast<uint4*>(p), make_uint4(bf16_two(v[0], v[1]), bf16_two(v[2], v[3]), bf16_two(v[4], v[5]), bf16_two(v[6], v[7])));
+  } else if (n == 8 && SBP_GUARD(p, 2) && SBP_GUARD(p + 7 * step, 2)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e * step] = __float2bfloat16_rn(v[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -130,18 +189,19 @@ __device__ __forceinline__ unsigned long long pair_mul(unsigned long long a, uns
   return v;
 }
 
-// The normal distribution Phi of two numbers, and e = exp(-z^2 / 2).  Below zero Phi(z) = e v(|z|), where v(t) = erfcx(t / sqrt 2) / 2
+// Of two numbers t = min(|z|, 16), e = exp(-t^2 / 2) and q = Phi(-t), the normal distribution's tail.  Phi(-t) = e v(t), where v(t) = erfcx(t / sqrt 2) / 2
 // falls off as 1 / t: it is k times a polynomial in k = 1 / (1 + 0.304 t) fitted to it for the smallest relative error (6e-8, over t up to
-// 13.6; with its roundings 4e-7), so the lower tail keeps its digits until e underflows.  Above zero it is 1 - Phi(-z).
-// From |z| = 16 on e is zero: what is larger, infinities too, is taken for 16.  NaN stays NaN.
+// 13.6; with its roundings 4e-7), so the tail keeps its digits until e underflows.
+// From t = 16 on e is zero: what is larger, infinities too, is taken for 16.  NaN stays NaN.
 // EXACT: z^2 is taken with what its rounding leaves, else its rounding is z^2 / 2 units in the last place of e (none for bf16 numbers).
 // Cost: two special functions and some eleven instructions a number, for which erfcf and expf take about sixty.
 template <bool EXACT>
-__device__ __forceinline__ void normal_two(float a, float b, unsigned long long& phi, unsigned long long& e) {
+__device__ __forceinline__ void tail_two(float a, float b, unsigned long long& t, unsigned long long& q, unsigned long long& e) {
   float ta, tb;
   asm("min.NaN.f32 %0, %1, 0f41800000;" : "=f"(ta) : "f"(fabsf(a)));
   asm("min.NaN.f32 %0, %1, 0f41800000;" : "=f"(tb) : "f"(fabsf(b)));
-  const unsigned long long t = pair_of(ta, tb), d = pair_fma(t, pair_of(0.30405593f), pair_of(1.0f));
+  t = pair_of(ta, tb);
+  const unsigned long long d = pair_fma(t, pair_of(0.30405593f), pair_of(1.0f));
   float ka, kb;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(ka) : "f"(pair_lo(d)));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(kb) : "f"(pair_hi(d)));
@@ -160,28 +220,26 @@ __device__ __forceinline__ void normal_two(float a, float b, unsigned long long&
   v = pair_fma(v, k, pair_of(0.10262408f));
   v = pair_fma(v, k, pair_of(0.12216413f));
   v = pair_fma(v, k, pair_of(0.12125883f));
-  v = pair_mul(pair_mul(v, k), e);
-  phi = pair_fma(v, pair_of(a < 0.f ? 1.f : -1.f, b < 0.f ? 1.f : -1.f), pair_of(a < 0.f ? 0.f : 1.f, b < 0.f ? 0.f : 1.f));      // (-0 is not below zero)
+  q = pair_mul(pair_mul(v, k), e);
 }
 
-// GeLU(z) = z Phi(z)
+// GeLU(z) = z Phi(z) = max(z, 0) - |z| Phi(-|z|): below zero the tail alone, with its digits.  (Minus infinity gives 0.)
 template <bool EXACT>
 __device__ __forceinline__ void gelu_two(float& a, float& b) {
-  unsigned long long phi, e;
-  normal_two<EXACT>(a, b, phi, e);
-  const unsigned long long y = pair_mul(pair_of(a, b), phi);
+  unsigned long long t, q, e;
+  tail_two<EXACT>(a, b, t, q, e);
+  const unsigned long long y = pair_fma(t ^ 0x8000000080000000ull, q, pair_of(fmaxf(a, 0.f), fmaxf(b, 0.f)));
   a = pair_lo(y);
   b = pair_hi(y);
 }
 
-// Its slope Phi(z) + z phi(z), phi(z) = e / sqrt(2 pi); |z| is taken for 16 at most where e is zero.
+// Its slope Phi(z) + z phi(z), phi(z) = e / sqrt(2 pi): with r = Phi(-t) - t phi(t), that is r below zero and 1 - r above.
 __device__ __forceinline__ void gelu_slope_two(float& a, float& b) {
-  unsigned long long phi, e;
-  normal_two<false>(a, b, phi, e);
-  const unsigned long long z = pair_of(fminf(fmaxf(a, -16.f), 16.f), fminf(fmaxf(b, -16.f), 16.f));
-  const unsigned long long y = pair_fma(pair_mul(z, e), pair_of(0.39894228f), phi);
-  a = pair_lo(y);
-  b = pair_hi(y);
+  unsigned long long t, q, e;
+  tail_two<false>(a, b, t, q, e);
+  const unsigned long long r = pair_fma(pair_mul(t, e), pair_of(-0.39894228f), q);
+  a = a < 0.f ? pair_lo(r) : 1.0f - pair_lo(r);
+  b = b < 0.f ? pair_hi(r) : 1.0f - pair_hi(r);
 }
 
 }  // namespace sbp

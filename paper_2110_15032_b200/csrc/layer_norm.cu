@@ -5,8 +5,10 @@
 // workspace, and a second kernel adds the blocks' up, always in the same order: P(sum), the all-reduce and the reduce-scatter of data
 // parallelism are which blocks it adds and where it stores.
 //
-// G threads share a row, each with NV times eight of its elements.  Rows too long for registers (over 16384) are read again for
+// G threads share a row, each with NV times eight of its elements.  Rows too long for registers (over 16384, backward 8192) are read again for
 // each pass, out of L2.
+#include <atomic>
+
 #include "blocks8.h"
 
 namespace sbp {
@@ -26,6 +28,7 @@ struct NormParams {
   const void* gamma;   // null: ones
   const void* beta;    // null: zeros
   int gamma_f32, beta_f32;
+  int gamma_whole, beta_whole;      // 16-byte aligned
   long long cols;
   float eps;
   float* parts;        // backward: [job * blocks of a job + block][2][cols]; null: the sums are not wanted
@@ -36,6 +39,18 @@ __device__ __forceinline__ float vector_at(const void* p, int f32, long long c, 
   if (!p) return none;
   if (f32) return SBP_GUARD(static_cast<const float*>(p) + c, 4) ? static_cast<const float*>(p)[c] : 0.f;
   return SBP_GUARD(static_cast<const __nv_bfloat16*>(p) + c, 2) ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[c]) : 0.f;
+}
+
+// Eight elements of gamma or beta; `whole`: they may be loaded as vectors.
+template <bool VEC>
+__device__ __forceinline__ void vector8(const void* p, int f32, int whole, long long col, int n, int step, float none, float (&v)[8]) {
+  if (VEC && whole && n > 0) {
+    if (f32) load8<true>(static_cast<const float*>(p) + col, v);
+    else load8<true>(static_cast<const __nv_bfloat16*>(p) + col, v);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < n ? vector_at(p, f32, col + e * step, none) : 0.f;
 }
 
 // Where thread t of G finds its elements of chunk i (8 G elements): VEC eight that follow one another, else every G-th.
@@ -77,9 +92,62 @@ __device__ __forceinline__ void row_sums(float (&s)[N], float (*buf)[N][32], int
 }
 
 constexpr int norm_threads(int g) { return g > 32 ? g : 256; }
+// Blocks an SM takes: what the registers of a row's elements and the next one's, gamma and beta leave, backward of grad_y's and the sums too.
+constexpr int blocks_per_sm(int g, int nv, bool backward) {
+  return !g ? (backward ? 2 : 3) : (backward ? (nv == 1 ? 768 : 512) : (nv == 1 ? 1024 : nv == 2 ? 768 : 512)) / norm_threads(g);
+}
+
+// Rows on their way: every thread copies its own elements of the rows that its block takes next into its own places in shared memory,
+// asynchronously, so that what is in flight does not hang on registers or barriers, and reads them back when their turn comes.  Q: 16-byte
+// quarters of a row's elements that a thread has.  (bf16 [8192, 4096]: a row ahead in registers 38.9 us, its backward pass 51.5.)
+__device__ __forceinline__ void copy16(unsigned to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+template <typename T, int G, int NV>
+__device__ __forceinline__ void fetch_row(unsigned char* slot, const T* row, int t, long long cols) {      // slot: [quarter][thread of the block]
+  constexpr int kQuarters = sizeof(T) / 2;   // of eight elements
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const Piece<G, true> at(i, t, cols);
+#pragma unroll
+    for (int k = 0; k < kQuarters; ++k) {
+      const T* from = row + at.col + k * (8 / kQuarters);
+      if (at.n > 0 && SBP_GUARD(from, 16)) copy16((unsigned)__cvta_generic_to_shared(slot + ((i * kQuarters + k) * norm_threads(G) + threadIdx.x) * 16), from);
+    }
+  }
+}
+template <typename T, int G, int NV>
+__device__ __forceinline__ void take_row(const unsigned char* slot, float (&v)[NV][8]) {
+  constexpr int kQuarters = sizeof(T) / 2;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if constexpr (kQuarters == 1) {
+      Eight<__nv_bfloat16, true> x;
+      x.a = *reinterpret_cast<const uint4*>(slot + (i * norm_threads(G) + threadIdx.x) * 16);
+      x.get(v[i]);
+    } else {
+      Eight<float, true> x;
+      x.a = *reinterpret_cast<const float4*>(slot + (2 * i * norm_threads(G) + threadIdx.x) * 16);
+      x.b = *reinterpret_cast<const float4*>(slot + ((2 * i + 1) * norm_threads(G) + threadIdx.x) * 16);
+      x.get(v[i]);
+    }
+  }
+}
+template <typename T>
+constexpr int row_bytes(int g, int nv) { return norm_threads(g) * nv * 8 * (int)sizeof(T); }
+// Rows that the ring holds, the one being worked on among them: as many as the blocks of an SM have room for, up to six.
+template <typename TX, typename TY>
+constexpr int ring_rows(int g, int nv, bool backward) {
+  const int room = 216 * 1024 / blocks_per_sm(g, nv, backward) / (row_bytes<TX>(g, nv) + (backward ? row_bytes<TY>(g, nv) : 0));
+  return room > 6 ? 6 : room;
+}
+template <typename TX, typename TY>
+constexpr int ring_bytes(int g, int nv, bool vec, bool backward) {
+  return vec ? ring_rows<TX, TY>(g, nv, backward) * (row_bytes<TX>(g, nv) + (backward ? row_bytes<TY>(g, nv) : 0)) : 0;
+}
 
 template <typename TX, typename TY, int G, int NV, bool VEC>
-__global__ void __launch_bounds__(norm_threads(G)) norm_kernel(const __grid_constant__ NormParams P) {
+__global__ void __launch_bounds__(norm_threads(G), blocks_per_sm(G, NV, false)) norm_kernel(const __grid_constant__ NormParams P) {
   constexpr int kGroups = norm_threads(G) / G;
   __shared__ float red[2][1][32];
   SBP_PDL_RELEASE();
@@ -91,20 +159,42 @@ __global__ void __launch_bounds__(norm_threads(G)) norm_kernel(const __grid_cons
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const Piece<G, VEC> at(i, t, P.cols);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      ga[i][e] = e < at.n ? vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f) : 0.f;
-      be[i][e] = e < at.n ? vector_at(P.beta, P.beta_f32, at.col + e * at.step, 0.f) : 0.f;
-    }
+    vector8<VEC>(P.gamma, P.gamma_f32, P.gamma_whole, at.col, at.n, at.step, 1.f, ga[i]);
+    vector8<VEC>(P.beta, P.beta_f32, P.beta_whole, at.col, at.n, at.step, 0.f, be[i]);
   }
   int turn = 0;
-  for (long long row = (long long)blockIdx.x * kGroups + threadIdx.x / G; row < J.rows; row += (long long)gridDim.x * kGroups) {
+  extern __shared__ __align__(16) unsigned char ring[];
+  constexpr int kRing = ring_rows<TX, TY>(G, NV, false);
+  static_assert(!VEC || kRing >= 3, "two rows ahead");
+  long long row = (long long)blockIdx.x * kGroups + threadIdx.x / G;
+  const long long stride = (long long)gridDim.x * kGroups;
+  auto fetch = [&](int slot, long long r) {
+    if (r < J.rows) fetch_row<TX, G, NV>(ring + slot * row_bytes<TX>(G, NV), static_cast<const TX*>(J.x) + r * J.ldx, t, P.cols);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) fetch(i, row + i * stride);
+  }
+  int slot = 0;
+  for (; row < J.rows; row += stride) {
     float v[NV][8];
     float s[1] = {0.f};
+    if constexpr (VEC) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
+      take_row<TX, G, NV>(ring + slot * row_bytes<TX>(G, NV), v);
+      fetch(slot == 0 ? kRing - 1 : slot - 1, row + (kRing - 1) * stride);
+      slot = slot + 1 == kRing ? 0 : slot + 1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const Piece<G, VEC> at(i, t, P.cols);
+        if (at.n > 0) load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, v[i], at.n, at.step);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const Piece<G, VEC> at(i, t, P.cols);
-      if (at.n > 0) load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, v[i], at.n, at.step);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (e < at.n) s[0] += v[i][e];
@@ -140,7 +230,7 @@ __global__ void __launch_bounds__(norm_threads(G)) norm_kernel(const __grid_cons
 }
 
 template <typename TX, typename TY, int G, int NV, bool VEC>
-__global__ void __launch_bounds__(norm_threads(G)) norm_grad_kernel(const __grid_constant__ NormParams P) {
+__global__ void __launch_bounds__(norm_threads(G), blocks_per_sm(G, NV, true)) norm_grad_kernel(const __grid_constant__ NormParams P) {
   constexpr int kGroups = norm_threads(G) / G;
   __shared__ float red[2][2][32];
   SBP_PDL_RELEASE();
@@ -152,24 +242,55 @@ __global__ void __launch_bounds__(norm_threads(G)) norm_grad_kernel(const __grid
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const Piece<G, VEC> at(i, t, P.cols);
+    vector8<VEC>(P.gamma, P.gamma_f32, P.gamma_whole, at.col, at.n, at.step, 1.f, ga[i]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      ga[i][e] = e < at.n ? vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f) : 0.f;
-      sum_g[i][e] = sum_b[i][e] = 0.f;
-    }
+    for (int e = 0; e < 8; ++e) sum_g[i][e] = sum_b[i][e] = 0.f;
   }
   int turn = 0;
-  for (long long row = (long long)blockIdx.x * kGroups + threadIdx.x / G; row < J.rows; row += (long long)gridDim.x * kGroups) {
-    float h[NV][8], d[NV][8];
+  extern __shared__ __align__(16) unsigned char ring[];
+  constexpr int kRing = ring_rows<TX, TY>(G, NV, true);
+  static_assert(!VEC || kRing >= 3, "two rows ahead");
+  constexpr int kSlot = row_bytes<TX>(G, NV) + row_bytes<TY>(G, NV);
+  long long row = (long long)blockIdx.x * kGroups + threadIdx.x / G;
+  const long long stride = (long long)gridDim.x * kGroups;
+  auto fetch = [&](int slot, long long r) {
+    if (r < J.rows) {
+      fetch_row<TX, G, NV>(ring + slot * kSlot, static_cast<const TX*>(J.x) + r * J.ldx, t, P.cols);
+      fetch_row<TY, G, NV>(ring + slot * kSlot + row_bytes<TX>(G, NV), static_cast<const TY*>(J.dy) + r * J.lddy, t, P.cols);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if constexpr (VEC) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const Piece<G, VEC> at(i, t, P.cols);
-      if (at.n > 0) {
-        load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, h[i], at.n, at.step);
-        load8<VEC>(static_cast<const TY*>(J.dy) + row * J.lddy + at.col, d[i], at.n, at.step);
+    for (int i = 0; i < kRing - 1; ++i) fetch(i, row + i * stride);
+  }
+  int slot = 0;
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto stats = [&](long long r) {
+    if (r < J.rows && SBP_GUARD(J.mean + r, 4)) next_mean = J.mean[r];
+    if (r < J.rows && SBP_GUARD(J.rstd + r, 4)) next_rstd = J.rstd[r];
+  };
+  stats(row);
+  for (; row < J.rows; row += stride) {
+    float h[NV][8], d[NV][8];
+    const float mean = next_mean, rstd = next_rstd;
+    stats(row + stride);
+    if constexpr (VEC) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
+      take_row<TX, G, NV>(ring + slot * kSlot, h);
+      take_row<TY, G, NV>(ring + slot * kSlot + row_bytes<TX>(G, NV), d);
+      fetch(slot == 0 ? kRing - 1 : slot - 1, row + (kRing - 1) * stride);
+      slot = slot + 1 == kRing ? 0 : slot + 1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const Piece<G, VEC> at(i, t, P.cols);
+        if (at.n > 0) {
+          load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, h[i], at.n, at.step);
+          load8<VEC>(static_cast<const TY*>(J.dy) + row * J.lddy + at.col, d[i], at.n, at.step);
+        }
       }
     }
-    const float mean = SBP_GUARD(J.mean + row, 4) ? J.mean[row] : 0.f, rstd = SBP_GUARD(J.rstd + row, 4) ? J.rstd[row] : 0.f;
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -348,7 +469,7 @@ __global__ void __launch_bounds__(kWideCols) norm_sums_wide_kernel(const __grid_
   store8<VEC>(part + P.cols + at.col, sum_b, at.n, at.step);
 }
 
-// The blocks' sums added up: 32 columns a block, its eight warps each every eighth part of an output, then the warps in order.
+// The blocks' sums added up: 32 columns a block, its sixteen warps each every sixteenth part of an output, then the warps in order.
 struct JoinParams {
   const float* parts;
   long long cols;
@@ -358,8 +479,9 @@ struct JoinParams {
   int replicas;                  // > 0: output 0 goes to so many buffers
   int split;                     // > 0: output 0 is split over so many shards
 };
-__global__ void __launch_bounds__(256) norm_join_kernel(const __grid_constant__ JoinParams P) {
-  __shared__ float sums[8][32];
+constexpr int kJoin = 16;
+__global__ void __launch_bounds__(32 * kJoin) norm_join_kernel(const __grid_constant__ JoinParams P) {
+  __shared__ float sums[kJoin][32];
   SBP_PDL_RELEASE();
   SBP_PDL_WAIT();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = blockIdx.y, z = blockIdx.z;
@@ -370,7 +492,7 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const __grid_constant__ 
     const int hi = P.hi[z] * P.per_job;
     const float* from = P.parts + which * P.cols + c;
 #pragma unroll 8
-    for (int i = P.lo[z] * P.per_job + warp; i < hi; i += 8)
+    for (int i = P.lo[z] * P.per_job + warp; i < hi; i += kJoin)
       if (SBP_GUARD(from + i * 2 * P.cols, 4)) v += from[i * 2 * P.cols];
   }
   sums[warp][lane] = v;
@@ -378,7 +500,7 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const __grid_constant__ 
   if (warp == 0 && c < P.cols) {
     v = sums[0][lane];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) v += sums[w][lane];
+    for (int w = 1; w < kJoin; ++w) v += sums[w][lane];
     if (P.split > 0) {
       int64_t start = 0, len = 0;
       int r = 0;
@@ -398,33 +520,27 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const __grid_constant__ 
   }
 }
 
-// Threads that share a row and chunks of eight elements each has, by the row's length; {0, 0}: the wide kernels.
+// Threads that share a row and chunks of eight elements each has, by the row's length; {0, 0}: the wide kernels (backward from 8193
+// elements on: x, grad_y and both sums of 32 elements a thread are more than 128 registers).
 struct NormForm {
   int g, nv;
 };
-NormForm norm_form(long long cols) {
+NormForm norm_form(long long cols, bool backward) {
   if (cols <= 256) return {32, 1};
   if (cols <= 512) return {32, 2};
   if (cols <= 1024) return {128, 1};
   if (cols <= 2048) return {128, 2};
   if (cols <= 4096) return {256, 2};
   if (cols <= 8192) return {512, 2};
-  if (cols <= 16384) return {512, 4};
+  if (cols <= 16384 && !backward) return {512, 4};
   return {0, 0};
 }
 
 // Blocks of a job: what the device holds, dealt out to the jobs, but no more than there are rows for.
 int norm_blocks(NormForm f, long long rows, int jobs, int per_sm) {
   const long long most = (rows * (f.g ? f.g : kWide) + norm_threads(f.g ? f.g : kWide) - 1) / norm_threads(f.g ? f.g : kWide);
-  const long long fair = ((long long)device_sms() * per_sm + jobs - 1) / jobs;
-  return (int)(most < fair ? most : fair);
-}
-
-// Blocks an SM takes: forward as many threads as the registers of a row's elements, gamma and beta leave, backward of twice the sums.
-int blocks_per_sm(NormForm f, bool backward) {
-  if (!f.g) return backward ? 2 : 3;
-  const int threads = norm_threads(f.g);
-  return (backward ? (f.nv == 4 ? 512 : f.nv == 2 ? 512 : 1024) : (f.nv == 4 ? 512 : 1024)) / threads;
+  const long long fair = (long long)device_sms() * per_sm / jobs;      // (one block more than the device holds is a second wave)
+  return (int)(most < fair ? most : fair > 1 ? fair : 1);
 }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -485,14 +601,33 @@ sbp_status check_vector(const sbp_tensor* t, const char* name, const sbp_tensor*
   return SBP_OK;
 }
 
+// One compiled form; a ring of more than 48 KiB has to be asked for, once a device.
+template <typename TX, typename TY, int G, int NV, bool VEC, bool BACKWARD>
+cudaError_t launch_one(const NormParams& P, int jobs, int blocks, cudaStream_t st) {
+  constexpr int kBytes = ring_bytes<TX, TY>(G, NV, VEC, BACKWARD);
+  void (*kernel)(NormParams);
+  if constexpr (BACKWARD) kernel = norm_grad_kernel<TX, TY, G, NV, VEC>;
+  else kernel = norm_kernel<TX, TY, G, NV, VEC>;
+  if constexpr (kBytes > 0) {
+    static std::atomic<unsigned long long> opted{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (dev >= 64 || !(opted.load(std::memory_order_relaxed) & bit)) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+      if (e != cudaSuccess) return e;
+      if (dev < 64) opted.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  return launch_dependent(kernel, dim3((unsigned)blocks, (unsigned)jobs), dim3(norm_threads(G)), (size_t)kBytes, st, P);
+}
 template <typename TX, typename TY, int G, int NV>
 cudaError_t launch_form(const NormParams& P, int jobs, int blocks, bool vec, bool backward, cudaStream_t st) {
-  const dim3 grid((unsigned)blocks, (unsigned)jobs), block(norm_threads(G));
-  if (backward)
-    return vec ? launch_dependent(norm_grad_kernel<TX, TY, G, NV, true>, grid, block, 0, st, P)
-               : launch_dependent(norm_grad_kernel<TX, TY, G, NV, false>, grid, block, 0, st, P);
-  return vec ? launch_dependent(norm_kernel<TX, TY, G, NV, true>, grid, block, 0, st, P)
-             : launch_dependent(norm_kernel<TX, TY, G, NV, false>, grid, block, 0, st, P);
+  if constexpr (NV < 4) {
+    if (backward) return vec ? launch_one<TX, TY, G, NV, true, true>(P, jobs, blocks, st) : launch_one<TX, TY, G, NV, false, true>(P, jobs, blocks, st);
+  }
+  return vec ? launch_one<TX, TY, G, NV, true, false>(P, jobs, blocks, st) : launch_one<TX, TY, G, NV, false, false>(P, jobs, blocks, st);
 }
 
 template <typename TX, typename TY>
@@ -519,7 +654,7 @@ sbp_status launch_norm(const NormParams& P, int jobs, int blocks, bool backward,
     if (backward) vec = vec && aligned16(j.dy) && j.lddy * sizeof(TY) % 16 == 0;
   }
   SBP_BOUNDS_UPLOAD(st);
-  const NormForm f = norm_form(P.cols);
+  const NormForm f = norm_form(P.cols, backward);
   cudaError_t e;
   switch (f.g * 8 + f.nv) {
     case 32 * 8 + 1: e = launch_form<TX, TY, 32, 1>(P, jobs, blocks, vec, backward, st); break;
@@ -546,7 +681,7 @@ sbp_status launch_typed(const NormParams& P, int jobs, int blocks, bool backward
 
 // Blocks a job gets in the backward pass of x, and the jobs whose sums the workspace holds: the same for the query and the call.
 int backward_blocks(const sbp_tensor* x, int* jobs) {
-  const NormForm f = norm_form(x->shape[x->ndim - 1]);
+  const NormForm f = norm_form(x->shape[x->ndim - 1], true);
   long long most = 0;
   *jobs = 0;
   for (int r = 0; r < placement_k(x); ++r) {
@@ -555,7 +690,7 @@ int backward_blocks(const sbp_tensor* x, int* jobs) {
     if (n > 0) ++*jobs;
   }
   if (*jobs && x->sbp[0].kind == SBP_BROADCAST) *jobs = 1;
-  return *jobs ? norm_blocks(f, most, *jobs, blocks_per_sm(f, true)) : 0;
+  return *jobs ? norm_blocks(f, most, *jobs, blocks_per_sm(f.g, f.nv, true)) : 0;
 }
 
 }  // namespace
@@ -583,6 +718,8 @@ sbp_status sbp_layer_norm(const sbp_tensor* x, const sbp_tensor* gamma, const sb
   P.beta = beta ? beta->local[0] : nullptr;
   P.gamma_f32 = gamma && gamma->dtype == SBP_F32;
   P.beta_f32 = beta && beta->dtype == SBP_F32;
+  P.gamma_whole = gamma && aligned16(P.gamma);
+  P.beta_whole = beta && aligned16(P.beta);
   P.cols = x->shape[x->ndim - 1];
   P.eps = eps;
   int n = 0;
@@ -610,8 +747,8 @@ sbp_status sbp_layer_norm(const sbp_tensor* x, const sbp_tensor* gamma, const sb
   SBP_BOUNDS_TENSOR(y);
   SBP_BOUNDS_TENSOR(mean);
   SBP_BOUNDS_TENSOR(rstd);
-  const NormForm f = norm_form(P.cols);
-  return launch_typed(P, n, n ? norm_blocks(f, most, n, blocks_per_sm(f, false)) : 0, false, x->dtype == SBP_F32, y->dtype == SBP_F32,
+  const NormForm f = norm_form(P.cols, false);
+  return launch_typed(P, n, n ? norm_blocks(f, most, n, blocks_per_sm(f.g, f.nv, false)) : 0, false, x->dtype == SBP_F32, y->dtype == SBP_F32,
                       static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -666,6 +803,7 @@ sbp_status sbp_layer_norm_backward(const sbp_tensor* x, const sbp_tensor* gamma,
   NormParams P{};
   P.gamma = gamma ? gamma->local[0] : nullptr;
   P.gamma_f32 = gamma && gamma->dtype == SBP_F32;
+  P.gamma_whole = gamma && aligned16(P.gamma);
   P.cols = x->shape[x->ndim - 1];
   P.parts = wanted ? static_cast<float*>(ws) : nullptr;
   P.first_only = x_b;
@@ -720,7 +858,7 @@ sbp_status sbp_layer_norm_backward(const sbp_tensor* x, const sbp_tensor* gamma,
   if (sig.kind == SBP_BROADCAST) Q.replicas = k;
   const dim3 grid((unsigned)((P.cols + 31) / 32), 2, partial ? (unsigned)k : 1u);
   SBP_BOUNDS_UPLOAD(stream);
-  const cudaError_t e = launch_dependent(norm_join_kernel, grid, dim3(256), 0, stream, Q);
+  const cudaError_t e = launch_dependent(norm_join_kernel, grid, dim3(32 * kJoin), 0, stream, Q);
   if (e != cudaSuccess) return cuda_fail(e, "layer norm gradient launch");
   count_launch();
   return SBP_OK;

@@ -58,7 +58,6 @@ struct Params8 {
   int tile_begin[SBP_MAX_K + 1], tiles_m[SBP_MAX_K], tiles_n[SBP_MAX_K];
   int n_rep, ngroups, nseg, chain, total_tiles;
   int a_tiles, b_tiles;                      // the scales are one for 128 rows (columns)
-  int per_column;                            // a scale a column, else one for 128 columns of a tile
   int y_tma;                                 // the copy engine can address the result
   int out_f32, swap;                         // swap: rows of the tile are columns of the result
   int splits;                                // CTAs of a cluster that share a tile's contraction
@@ -137,7 +136,8 @@ struct Shape8 {
   static constexpr int kColsCta = PAIR ? NB / 2 : NB;            // B rows this CTA loads
   static constexpr int kSlot = (kRows + kColsCta) * 128;
   static constexpr int kSlots = kRing / kSlot;                   // 5 (256 and 128 columns), 7, 8, 9
-  static constexpr int kAccs = NB == 256 ? 2 : 4, kAccCols = NB == 256 ? 256 : 128;
+  static constexpr int kAccs = NB == 256 ? 2 : 4, kAccCols = NB == 256 ? 256 : 128;                // accumulators in tensor memory, columns of one
+  static constexpr int kHalves = 1;              // accumulators of a block
   static constexpr int kScales = kGroup * (kRows + NB);          // floats of a slot: [row][block], [block][column]
   static constexpr int kAccWarps = 8;
   static constexpr int kCols = NB / (kAccWarps / 4);             // columns of an accumulating warp
@@ -208,7 +208,8 @@ __device__ __forceinline__ void store_one(const Params8& p, void* y, long long a
   }
 }
 
-template <bool PAIR, int NB, bool TMA>
+// COLS: a scale a column, else one for 128 columns of the tile.
+template <bool PAIR, int NB, bool TMA, bool COLS>
 __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_kernel(const __grid_constant__ Params8 p) {
   using C = Shape8<PAIR, NB, TMA>;
   constexpr int kCols = C::kCols, kAccWarps = C::kAccWarps, kRole = kAccWarps;      // the first warp behind the accumulators
@@ -285,58 +286,55 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
           ok = wait8(smem_addr(&bar_sc_full[ss]), s_round, abort_flag);
           if (!ok) break;
           rs4 = *reinterpret_cast<const float4*>(scales + ss * C::kScales + row * kGroup);
-          if (!p.per_column) {
+          if constexpr (!COLS) {
             const float4 cs = *reinterpret_cast<const float4*>(scales + ss * C::kScales + (kRows + part * kCols / 128) * kGroup);
             rs4 = make_float4(rs4.x * cs.x, rs4.y * cs.y, rs4.z * cs.z, rs4.w * cs.w);
           }
         }
         const float rs = j == 0 ? rs4.x : j == 1 ? rs4.y : j == 2 ? rs4.z : rs4.w;
-        ok = wait8(smem_addr(&bar_acc_full[a]), a_round, abort_flag);
-        if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + part * kCols;
-        constexpr int kStep = kCols < kLoad8 ? kCols : kLoad8;
-        // the last columns are in registers: the accumulator and the scales go back before they are added
-        auto hand_back = [&]() {
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) {
-            if constexpr (PAIR) mbar_arrive_cluster(acc_empty0 + a * 8);
-            else mbar_arrive(acc_empty0 + a * 8);
-          }
-        };
-        if (!p.per_column) {
+        const float* cs = scales + ss * C::kScales + kGroup * kRows + j * NB + part * kCols;
 #pragma unroll
-          for (int b = 0; b < kCols; b += kStep) {
+        for (int h = 0; h < C::kHalves; ++h) {
+          constexpr int kPart = kCols / C::kHalves, kStep = kPart < kLoad8 ? kPart : kLoad8;
+          ok = wait8(smem_addr(&bar_acc_full[a]), a_round, abort_flag);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + part * kPart;
+#pragma unroll
+          for (int b = 0; b < kPart; b += kStep) {
             float v[kStep];
             tmem_columns(at + b, v);
-            if (b + kStep == kCols) hand_back();
+            if (b + kStep == kPart) {              // the last columns are in registers: the accumulator goes back before they are added
+              asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) {
+                if constexpr (PAIR) mbar_arrive_cluster(acc_empty0 + a * 8);
+                else mbar_arrive(acc_empty0 + a * 8);
+              }
+            }
+            float* to = acc + h * kPart + b;
+            if constexpr (!COLS) {
 #pragma unroll
-            for (int i = 0; i < kStep; ++i) acc[b + i] = fmaf(v[i], rs, acc[b + i]);
-          }
-        } else {
-          const float* cs = scales + ss * C::kScales + kGroup * kRows + j * NB + part * kCols;
+              for (int i = 0; i < kStep; ++i) to[i] = fmaf(v[i], rs, to[i]);
+            } else {
 #pragma unroll
-          for (int b = 0; b < kCols; b += kStep) {
-            float v[kStep];
-            tmem_columns(at + b, v);
-            if (b + kStep == kCols) hand_back();
-#pragma unroll
-            for (int i = 0; i < kStep; i += 4) {
-              const float4 s = *reinterpret_cast<const float4*>(cs + b + i);
-              acc[b + i] = fmaf(v[i] * s.x, rs, acc[b + i]);
-              acc[b + i + 1] = fmaf(v[i + 1] * s.y, rs, acc[b + i + 1]);
-              acc[b + i + 2] = fmaf(v[i + 2] * s.z, rs, acc[b + i + 2]);
-              acc[b + i + 3] = fmaf(v[i + 3] * s.w, rs, acc[b + i + 3]);
+              for (int i = 0; i < kStep; i += 4) {
+                const float4 s = *reinterpret_cast<const float4*>(cs + h * kPart + b + i);
+                to[i] = fmaf(v[i] * s.x, rs, to[i]);
+                to[i + 1] = fmaf(v[i + 1] * s.y, rs, to[i + 1]);
+                to[i + 2] = fmaf(v[i + 2] * s.z, rs, to[i + 2]);
+                to[i + 3] = fmaf(v[i + 3] * s.w, rs, to[i + 3]);
+              }
             }
           }
+          if (++a == C::kAccs) { a = 0; a_round ^= 1; }
         }
+        if (!ok) break;
         if (j == kGroup - 1 || c + 1 == count) {
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_addr(&bar_sc_empty[ss]));
           if (++ss == kScaleSlots) { ss = 0; s_round ^= 1; }
         }
-        if (++a == C::kAccs) { a = 0; a_round ^= 1; }
       }
       if (!ok) break;
       const long long M = p.m[tc.g], N = p.n[tc.g], ldy = p.ldy[tc.g];
@@ -460,33 +458,38 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
         const bool leader = elect_one();
         int slot = 0, a = 0;
         unsigned round = 0, a_round = 0;
-        constexpr unsigned idesc = idesc8(kTileM, NB), lo = desc_lo_fixed(16), hi = desc_hi_fixed(1024);
+        constexpr unsigned idesc = idesc8(kTileM, NB / C::kHalves), lo = desc_lo_fixed(16), hi = desc_hi_fixed(1024);
         bool ok = true;
         for (int tile = first; tile < p.total_tiles && ok; tile += stride) {
           const Tile8 tc = tile_at(p, tile, kTileM, NB);
           const int count = blocks_of(p, tc.g, slice).count;
           for (int c = 0; c < count; ++c) {
             // (the operands are there as a rule: their wait comes first, off the chain)
-            ok = wait8(smem_addr(&bar_full[slot]), round, abort_flag) && wait8(smem_addr(&bar_acc_empty[a]), a_round ^ 1, abort_flag);
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            if (leader) {
-              const unsigned sa = smem_addr(smem + slot * C::kSlot), sb = sa + kRows * 128;
+            ok = wait8(smem_addr(&bar_full[slot]), round, abort_flag);
 #pragma unroll
-              for (int kk = 0; kk < 4; ++kk)       // 32 bytes of every row
-                umma8<PAIR>(tmem_base + a * C::kAccCols, desc_pack(lo + (sa >> 4) + kk * 2, hi), desc_pack(lo + (sb >> 4) + kk * 2, hi), idesc,
-                            kk == 0 ? 0u : 1u);
-              if constexpr (PAIR) {
-                umma_commit_pair(smem_addr(&bar_empty[slot]));
-                umma_commit_pair(smem_addr(&bar_acc_full[a]));
-              } else {
-                umma_commit_cta(smem_addr(&bar_empty[slot]));
-                umma_commit_cta(smem_addr(&bar_acc_full[a]));
+            for (int h = 0; h < C::kHalves && ok; ++h) {
+              ok = wait8(smem_addr(&bar_acc_empty[a]), a_round ^ 1, abort_flag);
+              if (!ok) break;
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              if (leader) {
+                const unsigned sa = smem_addr(smem + slot * C::kSlot), sb = sa + kRows * 128 + h * (C::kColsCta / C::kHalves) * 128;
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)     // 32 bytes of every row
+                  umma8<PAIR>(tmem_base + a * C::kAccCols, desc_pack(lo + (sa >> 4) + kk * 2, hi), desc_pack(lo + (sb >> 4) + kk * 2, hi), idesc,
+                              kk == 0 ? 0u : 1u);
+                if constexpr (PAIR) {
+                  if (h + 1 == C::kHalves) umma_commit_pair(smem_addr(&bar_empty[slot]));
+                  umma_commit_pair(smem_addr(&bar_acc_full[a]));
+                } else {
+                  umma_commit_cta(smem_addr(&bar_empty[slot]));
+                  umma_commit_cta(smem_addr(&bar_acc_full[a]));
+                }
               }
+              __syncwarp();
+              if (++a == C::kAccs) { a = 0; a_round ^= 1; }
             }
-            __syncwarp();
+            if (!ok) break;
             if (++slot == C::kSlots) { slot = 0; round ^= 1; }
-            if (++a == C::kAccs) { a = 0; a_round ^= 1; }
           }
         }
       }
@@ -518,7 +521,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
               const long long r = arow + t + i;
               copy(to + ((t + i) * kGroup + j) * 4, sa, sa + (p.a_tiles ? r >> 7 : r) * pitch, t + i < rows);
             }
-            if (p.per_column) {
+            if (COLS) {
 #pragma unroll
               for (int i = 0; i < NB; i += 64) {
                 const long long r = bcol + t + i;
@@ -604,7 +607,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
 }
 
 // Launch of one form, or (p null) the clusters of it that the current device holds at once.
-template <bool PAIR, int NB, bool TMA>
+template <bool PAIR, int NB, bool TMA, bool COLS>
 sbp_status launch8_form(const Params8* p, int cluster, int ctas, cudaStream_t st, int* capacity) {
   using C = Shape8<PAIR, NB, TMA>;
   static std::atomic<unsigned long long> opted{0};      // one bit per device
@@ -612,10 +615,10 @@ sbp_status launch8_form(const Params8* p, int cluster, int ctas, cudaStream_t st
   SBP_CUDA_TRY(cudaGetDevice(&dev));
   const unsigned long long bit = 1ull << (dev & 63);
   if (dev >= 64 || !(opted.load(std::memory_order_relaxed) & bit)) {
-    SBP_CUDA_TRY(cudaFuncSetAttribute(matmul8_kernel<PAIR, NB, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    SBP_CUDA_TRY(cudaFuncSetAttribute(matmul8_kernel<PAIR, NB, TMA, COLS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     if constexpr (PAIR) {      // the accumulators' registers come out of what the block was launched with
       cudaFuncAttributes attr;
-      SBP_CUDA_TRY(cudaFuncGetAttributes(&attr, matmul8_kernel<PAIR, NB, TMA>));
+      SBP_CUDA_TRY(cudaFuncGetAttributes(&attr, matmul8_kernel<PAIR, NB, TMA, COLS>));
       if (attr.numRegs < 168) return fail(SBP_ERR_UNSUPPORTED, "the 8-bit matmul kernel was built with %d registers a thread", attr.numRegs);
     }
     if (dev < 64) opted.fetch_or(bit, std::memory_order_relaxed);
@@ -636,11 +639,11 @@ sbp_status launch8_form(const Params8* p, int cluster, int ctas, cudaStream_t st
   cfg.numAttrs = p ? 2 : 1;
   if (!p) {
     cfg.gridDim = dim3((unsigned)(device_sms() / cluster * cluster));
-    SBP_CUDA_TRY(cudaOccupancyMaxActiveClusters(capacity, matmul8_kernel<PAIR, NB, TMA>, &cfg));
+    SBP_CUDA_TRY(cudaOccupancyMaxActiveClusters(capacity, matmul8_kernel<PAIR, NB, TMA, COLS>, &cfg));
     return SBP_OK;
   }
   SBP_BOUNDS_UPLOAD(st);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, matmul8_kernel<PAIR, NB, TMA>, *p);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, matmul8_kernel<PAIR, NB, TMA, COLS>, *p);
   if (e != cudaSuccess) return cuda_fail(e, "8-bit matmul launch");
   count_launch();
   return SBP_OK;
@@ -653,7 +656,7 @@ int pair_capacity() {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return device_sms() / 2;
   int n = known[dev].load(std::memory_order_relaxed);
   if (n == 0) {
-    if (launch8_form<true, 256, true>(nullptr, 2, 0, nullptr, &n) != SBP_OK || n < 1) {
+    if (launch8_form<true, 256, true, false>(nullptr, 2, 0, nullptr, &n) != SBP_OK || n < 1) {
       cudaGetLastError();
       n = device_sms() / 2;
     }
@@ -691,19 +694,19 @@ Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma) {
   return f;
 }
 
+template <bool COLS>
 sbp_status launch8(const Params8& p, Form8 f, bool tma, cudaStream_t st) {
-  const int ctas = f.pair ? 2 * std::min(p.total_tiles, pair_capacity()) : p.total_tiles * f.splits;
-  const int cluster = f.pair ? 2 : f.splits;
-  if (f.pair) return launch8_form<true, 256, true>(&p, cluster, ctas, st, nullptr);
+  if (f.pair) return launch8_form<true, 256, true, COLS>(&p, 2, 2 * std::min(p.total_tiles, pair_capacity()), st, nullptr);
+  const int ctas = p.total_tiles * f.splits;
   switch (f.nb + (tma ? 0 : 1)) {
-    case 16: return launch8_form<false, 16, true>(&p, cluster, ctas, st, nullptr);
-    case 17: return launch8_form<false, 16, false>(&p, cluster, ctas, st, nullptr);
-    case 32: return launch8_form<false, 32, true>(&p, cluster, ctas, st, nullptr);
-    case 33: return launch8_form<false, 32, false>(&p, cluster, ctas, st, nullptr);
-    case 64: return launch8_form<false, 64, true>(&p, cluster, ctas, st, nullptr);
-    case 65: return launch8_form<false, 64, false>(&p, cluster, ctas, st, nullptr);
-    case 128: return launch8_form<false, 128, true>(&p, cluster, ctas, st, nullptr);
-    default: return launch8_form<false, 128, false>(&p, cluster, ctas, st, nullptr);
+    case 16: return launch8_form<false, 16, true, COLS>(&p, f.splits, ctas, st, nullptr);
+    case 17: return launch8_form<false, 16, false, COLS>(&p, f.splits, ctas, st, nullptr);
+    case 32: return launch8_form<false, 32, true, COLS>(&p, f.splits, ctas, st, nullptr);
+    case 33: return launch8_form<false, 32, false, COLS>(&p, f.splits, ctas, st, nullptr);
+    case 64: return launch8_form<false, 64, true, COLS>(&p, f.splits, ctas, st, nullptr);
+    case 65: return launch8_form<false, 64, false, COLS>(&p, f.splits, ctas, st, nullptr);
+    case 128: return launch8_form<false, 128, true, COLS>(&p, f.splits, ctas, st, nullptr);
+    default: return launch8_form<false, 128, false, COLS>(&p, f.splits, ctas, st, nullptr);
   }
 }
 
@@ -757,7 +760,6 @@ sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const
   }
   for (int g = plan.ngroups; g <= SBP_MAX_K; ++g) p.tile_begin[g] = (int)tiles;
   p.total_tiles = (int)tiles;
-  p.per_column = !whole_blocks;
   if (tiles == 0) return SBP_OK;
   const int esz = p.out_f32 ? 4 : 2;
   bool y_tma = !f.swap && f.splits == 1;
@@ -787,7 +789,7 @@ sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const
         !tensor_map8(&p.map_b[s], p.b[s], cols, p.kseg[s], p.ldb[s], f.pair ? 128 : f.nb))
       return fail(SBP_ERR_CUDA, "cuTensorMapEncodeTiled failed for an operand of shard %d", s);
   }
-  return launch8(p, f, tma, st);
+  return whole_blocks ? launch8<false>(p, f, tma, st) : launch8<true>(p, f, tma, st);
 }
 
 }  // namespace

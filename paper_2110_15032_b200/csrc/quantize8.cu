@@ -18,117 +18,159 @@ struct Job8 {
 };
 struct Jobs8 {
   Job8 j[SBP_MAX_K];
-  int per_row_log;      // half-warps side by side along a row, log2 (row kernel)
+  int per_row_log;      // teams of eight lanes side by side along a row, log2 (row kernel)
+  int wide;             // 16-byte stores of values
 };
 
 enum { kQuantize = 0, kGelu = 1, kGeluGrad = 2 };
-constexpr int kRowsAtOnce = 4;      // rows a half-warp has in flight
+constexpr int kRowsAtOnce = 2;      // rows a team has in flight
 
-// Blocks of 128 along the rows: a half-warp a block, eight elements a lane, four rows in flight.
+// Blocks of 128 along the rows: a team of eight lanes a block, 16 elements a lane, two rows in flight.  (Eight elements a lane, 16 lanes a block: 13
+// instructions an element to quantise, 28 with GeLU, of which the conversions are 3 and GeLU 14; the rest is paid by lane and row.)
 template <typename TX, typename TY, int OP, bool VEC>
-__global__ void __launch_bounds__(256) blocks8_row_kernel(const __grid_constant__ Jobs8 P) {
+__global__ void __launch_bounds__(256, VEC && sizeof(TX) == 2 ? 4 : 3) blocks8_row_kernel(const __grid_constant__ Jobs8 P) {
   SBP_PDL_RELEASE();
   SBP_PDL_WAIT();
   const Job8& J = P.j[blockIdx.z];
-  const int hw = threadIdx.x >> 4, l = threadIdx.x & 15;
-  const int per_row = 1 << P.per_row_log;
-  const long long block = (long long)blockIdx.y * per_row + (hw & (per_row - 1));
-  const int rows_cta = 16 >> P.per_row_log;      // rows a pass of the CTA covers
-  const long long row0 = (long long)blockIdx.x * (rows_cta * kRowsAtOnce) + (hw >> P.per_row_log);
+  const int team = threadIdx.x >> 3, l = threadIdx.x & 7;
+  const long long block = ((long long)blockIdx.y << P.per_row_log) + (team & ((1 << P.per_row_log) - 1));
+  const int rows_cta = 32 >> P.per_row_log;      // rows a pass of the CTA covers
+  const long long row0 = (long long)blockIdx.x * (rows_cta * kRowsAtOnce) + (team >> P.per_row_log);
   const long long first = block * kBlock8;
-  const bool in_block = first < J.cols;
-  const int have = in_block ? (int)min((long long)kBlock8, J.cols - first) : 0;
-  // VEC: a lane's eight elements follow one another, all inside or all outside; else lanes take every sixteenth
-  const int step = VEC ? 1 : 16, at = VEC ? l * 8 : l;
-  const int n = VEC ? (at < have ? 8 : 0) : max(0, (have - l + 15) >> 4);
+  const int have = first < J.cols ? (int)min((long long)kBlock8, J.cols - first) : 0;
+  const int rows = (int)min((long long)(rows_cta * kRowsAtOnce), max(0LL, J.rows - row0));      // from this lane's first one on
+  // VEC: a lane's 16 elements follow one another, eight are all inside or all outside; else lanes take every eighth
+  constexpr int kStep = VEC ? 1 : 8, kNext = VEC ? 8 : 64;      // from one element to the next, from the first eight to the others
+  const int at = VEC ? l * 16 : l;
+  int n[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) n[k] = VEC ? (at + 8 * k < have ? 8 : 0) : min(8, max(0, (have - at - 64 * k + 7) >> 3));
   const long long col = first + at;
-  float v[kRowsAtOnce][8];
+  const TX* px = static_cast<const TX*>(J.x) + row0 * J.ldx + col;
+  unsigned char* pq = J.q + row0 * J.ldq + col;
+  TY* py = static_cast<TY*>(J.y) + (OP == kQuantize ? 0 : row0 * J.ldy + col);
+  float* ps = J.s + row0 * J.lds + block;
+  const long long hop_x = rows_cta * J.ldx, hop_q = rows_cta * J.ldq, hop_y = rows_cta * J.ldy, hop_s = rows_cta * J.lds;
+  Eight<TX, VEC> x[kRowsAtOnce][2];
 #pragma unroll
-  for (int i = 0; i < kRowsAtOnce; ++i) {
-    const long long row = row0 + i * rows_cta;
-    if (row < J.rows && n > 0) load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + col, v[i], n, step);
-    else {
+  for (int i = 0; i < kRowsAtOnce; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+    for (int k = 0; k < 2; ++k) {
+      x[i][k].clear();
+      if (i * rows_cta < rows && n[k] > 0) x[i][k].load(px + i * hop_x + k * kNext, n[k], kStep);
     }
-  }
   if constexpr (OP == kGeluGrad) {
-    unsigned char q[kRowsAtOnce][8];
+    uint2 q[kRowsAtOnce][2];
     float s[kRowsAtOnce];
 #pragma unroll
     for (int i = 0; i < kRowsAtOnce; ++i) {
-      const long long row = row0 + i * rows_cta;
-      const bool in = row < J.rows && n > 0;
-      const unsigned char* src = J.q + row * J.ldq + col;
-      const float* sp = J.s + row * J.lds + block;
-      s[i] = in && SBP_GUARD(sp, 4) ? *sp : 0.f;
-      if constexpr (VEC) {
-        *reinterpret_cast<uint2*>(q[i]) = in && SBP_GUARD(src, 8) ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
-      } else {
+      const bool in = i * rows_cta < rows && n[0] > 0;
+      const unsigned char* src = pq + i * hop_q;
+      s[i] = in && SBP_GUARD(ps + i * hop_s, 4) ? ps[i * hop_s] : 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) q[i][e] = in && e < n && SBP_GUARD(src + e * step, 1) ? src[e * step] : 0;
+      for (int k = 0; k < 2; ++k) {
+        q[i][k] = make_uint2(0u, 0u);
+        if constexpr (VEC) {
+          if (in && n[k] > 0 && SBP_GUARD(src + 8 * k, 8)) q[i][k] = *reinterpret_cast<const uint2*>(src + 8 * k);
+        } else if (in && n[k] == 8 && SBP_GUARD(src + k * kNext, 1) && SBP_GUARD(src + k * kNext + 7 * kStep, 1)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) (e < 4 ? q[i][k].x : q[i][k].y) |= (unsigned)src[k * kNext + e * kStep] << (8 * (e & 3));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (in && e < n[k] && SBP_GUARD(src + k * kNext + e * kStep, 1)) (e < 4 ? q[i][k].x : q[i][k].y) |= (unsigned)src[k * kNext + e * kStep] << (8 * (e & 3));
+        }
       }
     }
 #pragma unroll
-    for (int i = 0; i < kRowsAtOnce; ++i) {
-      const long long row = row0 + i * rows_cta;
-      if (row >= J.rows || n == 0) continue;
+    for (int i = 0; i < kRowsAtOnce; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        float a, b;
-        two_of_e4m3(q[i][e] | (unsigned)q[i][e + 1] << 8, a, b);
-        a *= s[i];
-        b *= s[i];
-        gelu_slope_two(a, b);
-        v[i][e] *= a;
-        v[i][e + 1] *= b;
+      for (int k = 0; k < 2; ++k) {
+        if (i * rows_cta >= rows || n[k] == 0) continue;
+        float v[8];
+        x[i][k].get(v);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          float a, b;
+          two_of_e4m3((e < 4 ? q[i][k].x : q[i][k].y) >> (8 * (e & 3)) & 0xffffu, a, b);
+          a *= s[i];
+          b *= s[i];
+          gelu_slope_two(a, b);
+          v[e] *= a;
+          v[e + 1] *= b;
+        }
+        store8<VEC>(py + i * hop_y + k * kNext, v, n[k], kStep);
       }
-      store8<VEC>(static_cast<TY*>(J.y) + row * J.ldy + col, v[i], n, step);
-    }
   } else {
 #pragma unroll
     for (int i = 0; i < kRowsAtOnce; ++i) {
-      const long long row = row0 + i * rows_cta;
-      unsigned m = 0;
+      unsigned m = max(largest_bits(x[i][0]), largest_bits(x[i][1]));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[i][e]) & 0x7fffffffu);
-#pragma unroll
-      for (int d = 1; d < 16; d <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
-      float c[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = v[i][e];
-      if (__any_sync(0xffffffffu, m >= 0x7f800000u)) {      // something is not finite: the maximum of the others
+      for (int d = 1; d < 8; d <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
+      const bool fix = __any_sync(0xffffffffu, m >= 0x7f800000u);      // something is not finite: the maximum of the others
+      if (fix) {
         m = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          m = max(m, finite_bits(v[i][e]));
-          c[e] = inf_to_nan(v[i][e]);
+        for (int k = 0; k < 2; ++k) {
+          float c[8];
+          x[i][k].get(c);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m = max(m, finite_bits(c[e]));
         }
 #pragma unroll
-        for (int d = 1; d < 16; d <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
+        for (int d = 1; d < 8; d <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
       }
-      if (row >= J.rows || n == 0) continue;
+      if (i * rows_cta >= rows || n[0] == 0) continue;
       const unsigned sb = scale_bits(m);
       const float inv = __uint_as_float(kInvBits - sb);
+      uint2 out[2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] *= inv;
-      const unsigned lo = e4m3_four(c), hi = e4m3_four(c + 4);
-      unsigned char* dst = J.q + row * J.ldq + col;
+      for (int k = 0; k < 2; ++k) {
+        float c[8];
+        x[i][k].get(c);
+        if (fix) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) c[e] = inf_to_nan(c[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const unsigned long long v = pair_mul(pair_of(c[e], c[e + 1]), pair_of(inv));
+          c[e] = pair_lo(v);
+          c[e + 1] = pair_hi(v);
+        }
+        out[k] = make_uint2(e4m3_four(c), e4m3_four(c + 4));
+      }
+      unsigned char* dst = pq + i * hop_q;
       if constexpr (VEC) {
-        if (SBP_GUARD(dst, 8)) *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+        if (P.wide) {
+          if (SBP_GUARD(dst, 16)) *reinterpret_cast<uint4*>(dst) = make_uint4(out[0].x, out[0].y, out[1].x, out[1].y);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            if (n[k] > 0 && SBP_GUARD(dst + 8 * k, 8)) *reinterpret_cast<uint2*>(dst + 8 * k) = out[k];
+        }
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < n && SBP_GUARD(dst + e * step, 1)) dst[e * step] = (unsigned char)((e < 4 ? lo : hi) >> (8 * (e & 3)));
+        for (int k = 0; k < 2; ++k)
+          if (n[k] == 8 && SBP_GUARD(dst + k * kNext, 1) && SBP_GUARD(dst + k * kNext + 7 * kStep, 1)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dst[k * kNext + e * kStep] = (unsigned char)((e < 4 ? out[k].x : out[k].y) >> (8 * (e & 3)));
+          } else
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < n[k] && SBP_GUARD(dst + k * kNext + e * kStep, 1)) dst[k * kNext + e * kStep] = (unsigned char)((e < 4 ? out[k].x : out[k].y) >> (8 * (e & 3)));
       }
-      float* sp = J.s + row * J.lds + block;
-      if (l == 0 && SBP_GUARD(sp, 4)) *sp = __uint_as_float(sb);
+      if (l == 0 && SBP_GUARD(ps + i * hop_s, 4)) ps[i * hop_s] = __uint_as_float(sb);
       if constexpr (OP == kGelu) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) c[e] = v[i][e];
+        for (int k = 0; k < 2; ++k) {
+          if (n[k] == 0) continue;
+          float c[8];
+          x[i][k].get(c);
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) gelu_two<sizeof(TX) == 4>(c[e], c[e + 1]);
-        store8<VEC>(static_cast<TY*>(J.y) + row * J.ldy + col, c, n, step);
+          for (int e = 0; e < 8; e += 2) gelu_two<sizeof(TX) == 4>(c[e], c[e + 1]);
+          store8<VEC>(py + i * hop_y + k * kNext, c, n[k], kStep);
+        }
       }
     }
   }
@@ -139,9 +181,11 @@ __global__ void __launch_bounds__(256) blocks8_row_kernel(const __grid_constant_
 // TRANS without TILES: a scale for each column of the tile.
 constexpr int kPitch8 = 33;                  // words of a transposed row in shared memory
 template <typename TX, bool TILES, bool TRANS, bool VEC>
-__global__ void __launch_bounds__(256) blocks8_tile_kernel(const __grid_constant__ Jobs8 P) {
+__global__ void __launch_bounds__(256, VEC && sizeof(TX) == 2 ? 3 : 2) blocks8_tile_kernel(const __grid_constant__ Jobs8 P) {
   __shared__ unsigned words[TRANS ? kBlock8 * kPitch8 : 1];
-  __shared__ unsigned amax[kBlock8];         // by column; TILES: by warp
+  constexpr bool kPacked = VEC && sizeof(TX) == 2;      // magnitudes of bf16 numbers, two to a word
+  __shared__ __align__(16) unsigned amax[8][TILES ? 1 : kPacked ? kBlock8 / 2 : kBlock8];      // by warp (and column)
+  __shared__ __align__(16) float inv_of[TILES ? 4 : kBlock8];
   SBP_PDL_RELEASE();
   SBP_PDL_WAIT();
   const Job8& J = P.j[blockIdx.z];
@@ -150,81 +194,145 @@ __global__ void __launch_bounds__(256) blocks8_tile_kernel(const __grid_constant
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cg = lane & 7, rq = warp * 4 + (lane >> 3);
   const int rows = (int)min((long long)kBlock8, J.rows - r0), cols = (int)min((long long)kBlock8, J.cols - c0);
-  float v[2][4][8];
+  Eight<TX, VEC> x[2][4];
 #pragma unroll
   for (int g = 0; g < 2; ++g)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = rq * 4 + i, c = g * 64 + cg * 8, n = r < rows ? min(8, cols - c) : 0;
-      if (n > 0) load8<VEC>(static_cast<const TX*>(J.x) + (r0 + r) * J.ldx + c0 + c, v[g][i], n);
-      else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[g][i][e] = 0.f;
-      }
+      x[g][i].clear();
+      if (n > 0) x[g][i].load(static_cast<const TX*>(J.x) + (r0 + r) * J.ldx + c0 + c, n, 1);
     }
+  // The scale of the tile (of every column).  First the largest magnitude of all; where that is not finite, of what is.
+  float inv = 0.f;
+  bool fix = false;
   if constexpr (TILES) {
     unsigned m = 0;
 #pragma unroll
     for (int g = 0; g < 2; ++g)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i) m = max(m, largest_bits(x[g][i]));
+    fix = __syncthreads_or(m >= 0x7f800000u);
+    if (fix) {
+      m = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, finite_bits(v[g][i][e]));
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float v[8];
+          x[g][i].get(v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m = max(m, finite_bits(v[e]));
+        }
+    }
     m = __reduce_max_sync(0xffffffffu, m);
-    if (lane == 0) amax[warp] = m;
+    if (lane == 0) amax[warp][0] = m;
     __syncthreads();
-    m = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) m = max(m, amax[w]);
+    for (int w = 0; w < 8; ++w) m = max(m, amax[w][0]);
     const unsigned sb = scale_bits(m);
-    const float inv = __uint_as_float(kInvBits - sb);
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[g][i][e] = inf_to_nan(v[g][i][e]) * inv;
+    inv = __uint_as_float(kInvBits - sb);
     if (threadIdx.x == 0) {
       float* sp = J.s + (TRANS ? (long long)blockIdx.y * J.lds + blockIdx.x : (long long)blockIdx.x * J.lds + blockIdx.y);
       if (SBP_GUARD(sp, 4)) *sp = __uint_as_float(sb);
     }
   } else {
-    if (threadIdx.x < kBlock8) amax[threadIdx.x] = 0u;
-    __syncthreads();
+    auto columns = [&](bool finite_only) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+      for (int g = 0; g < 2; ++g) {
+        constexpr int kWords = kPacked ? 4 : 8;
+        unsigned m[kWords] = {};
+        if constexpr (kPacked) {
+          auto pairs = [&](int i, int w) {       // magnitudes of two columns
+            const uint4& a = x[g][i].a;
+            unsigned v = (w == 0 ? a.x : w == 1 ? a.y : w == 2 ? a.z : a.w) & 0x7fff7fffu;
+            if (finite_only) {
+              if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+              if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
+            }
+            return v;
+          };
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        unsigned m = 0;
+          for (int w = 0; w < 4; ++w) m[w] = __vmaxs2(__vimax3_s16x2(pairs(0, w), pairs(1, w), pairs(2, w)), pairs(3, w));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m = max(m, finite_bits(v[g][i][e]));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 16));
-        if (lane < 8) atomicMax(&amax[g * 64 + cg * 8 + e], m);
+          for (int w = 0; w < 4; ++w) {
+            m[w] = __vmaxs2(m[w], __shfl_xor_sync(0xffffffffu, m[w], 8));
+            m[w] = __vmaxs2(m[w], __shfl_xor_sync(0xffffffffu, m[w], 16));
+          }
+          if (lane < 8) *reinterpret_cast<uint4*>(&amax[warp][g * 32 + cg * 4]) = make_uint4(m[0], m[1], m[2], m[3]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v[8];
+            x[g][i].get(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m[e] = max(m[e], finite_only ? finite_bits(v[e]) : __float_as_uint(v[e]) & 0x7fffffffu);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            m[e] = max(m[e], __shfl_xor_sync(0xffffffffu, m[e], 8));
+            m[e] = max(m[e], __shfl_xor_sync(0xffffffffu, m[e], 16));
+          }
+          if (lane < 8) {
+            *reinterpret_cast<uint4*>(&amax[warp][g * 64 + cg * 8]) = make_uint4(m[0], m[1], m[2], m[3]);
+            *reinterpret_cast<uint4*>(&amax[warp][g * 64 + cg * 8 + 4]) = make_uint4(m[4], m[5], m[6], m[7]);
+          }
+        }
       }
-    __syncthreads();
+      __syncthreads();
+      unsigned m = 0;
+      if (threadIdx.x < kBlock8) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float inv = __uint_as_float(kInvBits - scale_bits(amax[g * 64 + cg * 8 + e]));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[g][i][e] = inf_to_nan(v[g][i][e]) * inv;
+        for (int w = 0; w < 8; ++w) {
+          if constexpr (kPacked) m = max(m, (amax[w][threadIdx.x >> 1] >> (16 * (threadIdx.x & 1)) & 0xffffu) << 16);
+          else m = max(m, amax[w][threadIdx.x]);
+        }
+        const unsigned sb = scale_bits(m);
+        inv_of[threadIdx.x] = __uint_as_float(kInvBits - sb);
+        float* sp = J.s + (c0 + threadIdx.x) * J.lds + blockIdx.x;
+        if (threadIdx.x < cols && m < 0x7f800000u && SBP_GUARD(sp, 4)) *sp = __uint_as_float(sb);
       }
-    if (threadIdx.x < cols) {
-      float* sp = J.s + (c0 + threadIdx.x) * J.lds + blockIdx.x;
-      if (SBP_GUARD(sp, 4)) *sp = __uint_as_float(scale_bits(amax[threadIdx.x]));
+      return m >= 0x7f800000u;
+    };
+    fix = __syncthreads_or(columns(false));
+    if (fix) {
+      columns(true);
+      __syncthreads();
     }
   }
+  // element e of rows 0..3 of a group of columns, scaled
+  auto scaled = [&](int g, float (&v)[4][8]) {
+    float s[8];
+    if constexpr (!TILES) {
+      *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(&inv_of[g * 64 + cg * 8]);
+      *reinterpret_cast<float4*>(s + 4) = *reinterpret_cast<const float4*>(&inv_of[g * 64 + cg * 8 + 4]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[g][i].get(v[i]);
+      if (fix) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = inf_to_nan(v[i][e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const unsigned long long w = pair_mul(pair_of(v[i][e], v[i][e + 1]), TILES ? pair_of(inv) : pair_of(s[e], s[e + 1]));
+        v[i][e] = pair_lo(w);
+        v[i][e + 1] = pair_hi(w);
+      }
+    }
+  };
   if constexpr (!TRANS) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < 2; ++g) {
+      float v[4][8];
+      scaled(g, v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = rq * 4 + i, c = g * 64 + cg * 8, n = r < rows ? min(8, cols - c) : 0;
         if (n <= 0) continue;
         unsigned char* dst = J.q + (r0 + r) * J.ldq + c0 + c;
-        const unsigned lo = e4m3_four(v[g][i]), hi = e4m3_four(v[g][i] + 4);
+        const unsigned lo = e4m3_four(v[i]), hi = e4m3_four(v[i] + 4);
         if constexpr (VEC) {
           if (SBP_GUARD(dst, 8)) *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
         } else {
@@ -233,14 +341,18 @@ __global__ void __launch_bounds__(256) blocks8_tile_kernel(const __grid_constant
             if (e < n && SBP_GUARD(dst + e, 1)) dst[e] = (unsigned char)((e < 4 ? lo : hi) >> (8 * (e & 3)));
         }
       }
+    }
   } else {
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < 2; ++g) {
+      float v[4][8];
+      scaled(g, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float f[4] = {v[g][0][e], v[g][1][e], v[g][2][e], v[g][3][e]};
+        const float f[4] = {v[0][e], v[1][e], v[2][e], v[3][e]};
         words[(g * 64 + cg * 8 + e) * kPitch8 + rq] = e4m3_four(f);
       }
+    }
     __syncthreads();
     // a warp a row of the result at a time, four values a lane
     const bool whole = (reinterpret_cast<unsigned long long>(J.q) & 3) == 0 && (J.ldq & 3) == 0;
@@ -297,18 +409,20 @@ int make_jobs(const sbp_tensor* x, const sbp_tensor* y, const sbp_tensor* q, con
 template <typename TX, typename TY, int OP>
 sbp_status launch_rows(Jobs8& P, int n, cudaStream_t st) {
   if (n == 0) return SBP_OK;
-  bool vec = true;
+  bool vec = true, wide = true;
   long long rows = 0, blocks = 0;
   for (int i = 0; i < n; ++i) {
     const Job8& j = P.j[i];
     vec = vec && aligned(j.x, 16) && j.ldx * sizeof(TX) % 16 == 0 && aligned(j.q, 8) && j.ldq % 8 == 0 && j.cols % 8 == 0;
+    wide = wide && aligned(j.q, 16) && j.ldq % 16 == 0 && j.cols % 16 == 0;
     if (OP != kQuantize) vec = vec && aligned(j.y, 16) && j.ldy * sizeof(TY) % 16 == 0;
     rows = j.rows > rows ? j.rows : rows;
     blocks = blocks8(j.cols) > blocks ? blocks8(j.cols) : blocks;
   }
+  P.wide = wide;
   P.per_row_log = 0;
-  while (P.per_row_log < 4 && (1 << P.per_row_log) < blocks) ++P.per_row_log;
-  const long long rows_cta = (16 >> P.per_row_log) * kRowsAtOnce;
+  while (P.per_row_log < 5 && (1 << P.per_row_log) < blocks) ++P.per_row_log;
+  const long long rows_cta = (32 >> P.per_row_log) * kRowsAtOnce;
   const long long gx = (rows + rows_cta - 1) / rows_cta, gy = (blocks + (1 << P.per_row_log) - 1) >> P.per_row_log;
   if (gx > 0x7fffffffLL || gy > 65535) return fail(SBP_ERR_UNSUPPORTED, "tensor too large for one launch");
   const dim3 grid((unsigned)gx, (unsigned)gy, (unsigned)n);

@@ -25,7 +25,7 @@ def half_step(dtype):
 
 
 def depth(cols):
-    chunks = 4 if cols <= 16384 else -(-cols // 4096)
+    chunks = max(4, -(-cols // 4096))                # a chunk of the longest rows is 4096 elements
     return 8 * chunks + 16
 
 
