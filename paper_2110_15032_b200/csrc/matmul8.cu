@@ -37,7 +37,6 @@ bool tensor_map8_out(CUtensorMap* map, const void* base, int esz, long long rows
 namespace {
 
 constexpr int kRows = 128;                   // rows of the A operand a CTA holds
-constexpr int kRing = 168 * 1024;
 constexpr int kScaleSlots = 3, kGroup = 4;   // slots of the scales' ring, blocks whose scales share one
 constexpr int kLoad8 = 32;                   // accumulator columns loaded at a time
 constexpr int kPanel = 8;                    // row tiles walked together
@@ -59,6 +58,7 @@ struct Params8 {
   int n_rep, ngroups, nseg, chain, total_tiles;
   int a_tiles, b_tiles;                      // the scales are one for 128 rows (columns)
   int y_tma;                                 // the copy engine can address the result
+  int y_align;                               // bytes that every row of the result (and of its replicas) is aligned to, 16 at most
   int out_f32, swap;                         // swap: rows of the tile are columns of the result
   int splits;                                // CTAs of a cluster that share a tile's contraction
 };
@@ -135,13 +135,16 @@ template <bool PAIR, int NB, bool TMA>
 struct Shape8 {
   static constexpr int kColsCta = PAIR ? NB / 2 : NB;            // B rows this CTA loads
   static constexpr int kSlot = (kRows + kColsCta) * 128;
-  static constexpr int kSlots = kRing / kSlot;                   // 5 (256 and 128 columns), 7, 8, 9
-  static constexpr int kAccs = NB == 256 ? 2 : 4, kAccCols = NB == 256 ? 256 : 128;                // accumulators in tensor memory, columns of one
-  static constexpr int kHalves = 1;              // accumulators of a block
+  static constexpr int kCtas = NB <= 32 && TMA ? 2 : 1;          // of an SM: narrow tiles leave room for the next tile's, or the next product's
+  static constexpr int kSlots = NB == 16 ? 5 : NB == 32 ? 4 : (168 * 1024) / kSlot;      // 5 (256 and 128 columns), 7, 4, 5
+  static constexpr int kAccs = NB == 256 ? 2 : 4;                // accumulators in tensor memory
+  static constexpr int kAccCols = NB == 256 ? 256 : NB <= 32 ? 32 : 128;      // columns of one
+  static constexpr int kTmem = kAccs * kAccCols;
   static constexpr int kScales = kGroup * (kRows + NB);          // floats of a slot: [row][block], [block][column]
   static constexpr int kAccWarps = 8;
   static constexpr int kCols = NB / (kAccWarps / 4);             // columns of an accumulating warp
-  static constexpr int kSlab = 32 * 128;                         // its staging: 32 rows of 128 bytes
+  static constexpr int kSlabRow = kCols * 4 < 128 ? kCols * 4 : 128;      // its staging: 32 rows of so many bytes
+  static constexpr int kSlab = 32 * kSlabRow;
   static constexpr int kThreads = (kAccWarps + (TMA ? 4 : 8)) * 32;
   static constexpr int kSmem = kSlots * kSlot + kAccWarps * kSlab + kScaleSlots * kScales * 4 + 1024;
 };
@@ -210,7 +213,7 @@ __device__ __forceinline__ void store_one(const Params8& p, void* y, long long a
 
 // COLS: a scale a column, else one for 128 columns of the tile.
 template <bool PAIR, int NB, bool TMA, bool COLS>
-__global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_kernel(const __grid_constant__ Params8 p) {
+__global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, NB, TMA>::kCtas) matmul8_kernel(const __grid_constant__ Params8 p) {
   using C = Shape8<PAIR, NB, TMA>;
   constexpr int kCols = C::kCols, kAccWarps = C::kAccWarps, kRole = kAccWarps;      // the first warp behind the accumulators
   constexpr int kTileM = PAIR ? 256 : 128;
@@ -245,10 +248,10 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
   }
   if (warp == kRole + 1) {
     if constexpr (PAIR) {
-      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_slot)), "r"(512) : "memory");
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_slot)), "r"(C::kTmem) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     } else {
-      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_slot)), "r"(512) : "memory");
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base_slot)), "r"(C::kTmem) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
   }
@@ -293,18 +296,17 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
         }
         const float rs = j == 0 ? rs4.x : j == 1 ? rs4.y : j == 2 ? rs4.z : rs4.w;
         const float* cs = scales + ss * C::kScales + kGroup * kRows + j * NB + part * kCols;
-#pragma unroll
-        for (int h = 0; h < C::kHalves; ++h) {
-          constexpr int kPart = kCols / C::kHalves, kStep = kPart < kLoad8 ? kPart : kLoad8;
+        {
+          constexpr int kStep = kCols < kLoad8 ? kCols : kLoad8;
           ok = wait8(smem_addr(&bar_acc_full[a]), a_round, abort_flag);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + part * kPart;
+          const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + part * kCols;
 #pragma unroll
-          for (int b = 0; b < kPart; b += kStep) {
+          for (int b = 0; b < kCols; b += kStep) {
             float v[kStep];
             tmem_columns(at + b, v);
-            if (b + kStep == kPart) {              // the last columns are in registers: the accumulator goes back before they are added
+            if (b + kStep == kCols) {              // the last columns are in registers: the accumulator goes back before they are added
               asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
               __syncwarp();
               if (lane == 0) {
@@ -312,14 +314,14 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
                 else mbar_arrive(acc_empty0 + a * 8);
               }
             }
-            float* to = acc + h * kPart + b;
+            float* to = acc + b;
             if constexpr (!COLS) {
 #pragma unroll
               for (int i = 0; i < kStep; ++i) to[i] = fmaf(v[i], rs, to[i]);
             } else {
 #pragma unroll
               for (int i = 0; i < kStep; i += 4) {
-                const float4 s = *reinterpret_cast<const float4*>(cs + h * kPart + b + i);
+                const float4 s = *reinterpret_cast<const float4*>(cs + b + i);
                 to[i] = fmaf(v[i] * s.x, rs, to[i]);
                 to[i + 1] = fmaf(v[i + 1] * s.y, rs, to[i + 1]);
                 to[i + 2] = fmaf(v[i + 2] * s.z, rs, to[i + 2]);
@@ -329,7 +331,6 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
           }
           if (++a == C::kAccs) { a = 0; a_round ^= 1; }
         }
-        if (!ok) break;
         if (j == kGroup - 1 || c + 1 == count) {
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_addr(&bar_sc_empty[ss]));
@@ -341,10 +342,10 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
       const int n_out = (tc.g == 0 ? p.n_rep : 0) + 1;
       const long long row0 = tc.m0 + (int)rank * kRows, col0 = tc.n0 + part * kCols;
       if (splits > 1) {                            // the partial tile, for the cluster to add up; the ring is done with
-        float* mine = reinterpret_cast<float*>(smem) + row * (NB + 1) + part * kCols;
+        float* mine = reinterpret_cast<float*>(smem) + row * (NB + 4) + part * kCols;
         asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < kCols; ++i) mine[i] = acc[i];
+        for (int i = 0; i < kCols; i += 4) *reinterpret_cast<float4*>(mine + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
       } else if (p.swap) {                         // neighbouring lanes are neighbouring columns of the result
         const long long n = row0 + row;
 #pragma unroll
@@ -355,6 +356,8 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
       } else {
         // through a slab of shared memory, so that a warp stores whole pieces of rows
         unsigned char* slab = staging + warp * C::kSlab;
+        constexpr int kMask = C::kSlabRow / 16 - 1;
+        auto at_chunk = [&](int r, int c) { return slab + r * C::kSlabRow + ((c ^ (r & kMask)) << 4); };      // 16 bytes
         auto rows_out = [&](auto f32_tag) {
           constexpr bool F32 = decltype(f32_tag)::value;
           constexpr int esz = F32 ? 4 : 2, kPiece = kCols < 128 / esz ? kCols : 128 / esz, kChunks = kPiece * esz / 16;
@@ -373,7 +376,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
               uint4 o;
               if constexpr (F32) o = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
               else o = make_uint4(bf16_two(f[0], f[1]), bf16_two(f[2], f[3]), bf16_two(f[4], f[5]), bf16_two(f[6], f[7]));
-              *reinterpret_cast<uint4*>(slab + lane * 128 + ((c ^ (lane & 7)) << 4)) = o;
+              *reinterpret_cast<uint4*>(at_chunk(lane, c)) = o;
             }
             if (kChunks == 8 && p.y_tma) {         // a whole slab
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -385,24 +388,32 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
               continue;
             }
             __syncwarp();
-            for (int i = 0; i < kChunks; ++i) {
-              const int r = i * (32 / kChunks) + lane / kChunks, c = lane % kChunks;
-              const long long m = m0 + r, n = n0 + c * kPer;
-              if (m >= M || n >= N) continue;
-              const unsigned char* from = slab + r * 128 + ((c ^ (r & 7)) << 4);
-              for (int o = 0; o < n_out; ++o) {
-                unsigned char* to = static_cast<unsigned char*>(o == 0 ? p.y[tc.g] : p.y_rep[o - 1]) + (m * ldy + n) * esz;
-                if (p.y_tma && n + kPer <= N) {    // (that also says that whole vectors are aligned)
-                  if (SBP_GUARD(to, 16)) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
-                } else {
-                  for (int e = 0; e < kPer && n + e < N; ++e) {
-                    if (!SBP_GUARD(to + e * esz, esz)) continue;
-                    if constexpr (F32) *reinterpret_cast<float*>(to + e * 4) = *reinterpret_cast<const float*>(from + e * 4);
-                    else *reinterpret_cast<unsigned short*>(to + e * 2) = *reinterpret_cast<const unsigned short*>(from + e * 2);
+            auto stores = [&](auto unit_tag) {     // pieces of `unit` bytes, neighbouring lanes neighbouring ones
+              using Unit = decltype(unit_tag);
+              constexpr int unit = sizeof(Unit), kUnits = kPiece * esz / unit, kElems = unit / esz;
+              for (int i = lane; i < 32 * kUnits; i += 32) {
+                const int r = i / kUnits, u = i % kUnits;
+                const long long m = m0 + r, n = n0 + u * kElems;
+                if (m >= M || n >= N) continue;
+                const unsigned char* from = at_chunk(r, u * unit / 16) + u * unit % 16;
+                for (int o = 0; o < n_out; ++o) {
+                  unsigned char* to = static_cast<unsigned char*>(o == 0 ? p.y[tc.g] : p.y_rep[o - 1]) + (m * ldy + n) * esz;
+                  if (n + kElems <= N) {
+                    if (SBP_GUARD(to, unit)) *reinterpret_cast<Unit*>(to) = *reinterpret_cast<const Unit*>(from);
+                  } else {
+                    for (int e = 0; e < kElems && n + e < N; ++e) {
+                      if (!SBP_GUARD(to + e * esz, esz)) continue;
+                      if constexpr (F32) *reinterpret_cast<float*>(to + e * 4) = *reinterpret_cast<const float*>(from + e * 4);
+                      else *reinterpret_cast<unsigned short*>(to + e * 2) = *reinterpret_cast<const unsigned short*>(from + e * 2);
+                    }
                   }
                 }
               }
-            }
+            };
+            if (p.y_align == 16) stores(uint4{});
+            else if (p.y_align == 8) stores(uint2{});
+            else if (F32 || p.y_align == 4) stores(unsigned{});
+            else stores((unsigned short)0);
           }
         };
         if (p.out_f32) rows_out(std::true_type{});
@@ -458,7 +469,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
         const bool leader = elect_one();
         int slot = 0, a = 0;
         unsigned round = 0, a_round = 0;
-        constexpr unsigned idesc = idesc8(kTileM, NB / C::kHalves), lo = desc_lo_fixed(16), hi = desc_hi_fixed(1024);
+        constexpr unsigned idesc = idesc8(kTileM, NB), lo = desc_lo_fixed(16), hi = desc_hi_fixed(1024);
         bool ok = true;
         for (int tile = first; tile < p.total_tiles && ok; tile += stride) {
           const Tile8 tc = tile_at(p, tile, kTileM, NB);
@@ -466,19 +477,18 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
           for (int c = 0; c < count; ++c) {
             // (the operands are there as a rule: their wait comes first, off the chain)
             ok = wait8(smem_addr(&bar_full[slot]), round, abort_flag);
-#pragma unroll
-            for (int h = 0; h < C::kHalves && ok; ++h) {
-              ok = wait8(smem_addr(&bar_acc_empty[a]), a_round ^ 1, abort_flag);
-              if (!ok) break;
+            ok = ok && wait8(smem_addr(&bar_acc_empty[a]), a_round ^ 1, abort_flag);
+            if (!ok) break;
+            {
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               if (leader) {
-                const unsigned sa = smem_addr(smem + slot * C::kSlot), sb = sa + kRows * 128 + h * (C::kColsCta / C::kHalves) * 128;
+                const unsigned sa = smem_addr(smem + slot * C::kSlot), sb = sa + kRows * 128;
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)     // 32 bytes of every row
                   umma8<PAIR>(tmem_base + a * C::kAccCols, desc_pack(lo + (sa >> 4) + kk * 2, hi), desc_pack(lo + (sb >> 4) + kk * 2, hi), idesc,
                               kk == 0 ? 0u : 1u);
                 if constexpr (PAIR) {
-                  if (h + 1 == C::kHalves) umma_commit_pair(smem_addr(&bar_empty[slot]));
+                  umma_commit_pair(smem_addr(&bar_empty[slot]));
                   umma_commit_pair(smem_addr(&bar_acc_full[a]));
                 } else {
                   umma_commit_cta(smem_addr(&bar_empty[slot]));
@@ -488,7 +498,6 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
               __syncwarp();
               if (++a == C::kAccs) { a = 0; a_round ^= 1; }
             }
-            if (!ok) break;
             if (++slot == C::kSlots) { slot = 0; round ^= 1; }
           }
         }
@@ -578,19 +587,49 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
         const Tile8 tc = tile_at(p, first, kTileM, NB);
         const long long M = p.m[tc.g], N = p.n[tc.g], ldy = p.ldy[tc.g];
         const int n_out = (tc.g == 0 ? p.n_rep : 0) + 1;
-        const int lo = kRows * NB * slice / splits, hi = kRows * NB * (slice + 1) / splits;
+        // four columns at a time: neighbouring threads take neighbouring columns of the result, which are rows of the tile where the
+        // operands are exchanged
+        constexpr int kQuads = NB / 4;
+        const int lo = kRows * kQuads * slice / splits, hi = kRows * kQuads * (slice + 1) / splits;
         for (int e = lo + tid; e < hi; e += kAccWarps * 32) {
-          const int r = p.swap ? e & (kRows - 1) : e / NB, c = p.swap ? e / kRows : e % NB;
-          const unsigned at = smem_addr(smem) + (unsigned)(r * (NB + 1) + c) * 4;
-          float v = 0.f;
-          for (int s = 0; s < splits; ++s) {
-            float x;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(map_to_cta(at, s)) : "memory");
-            v = s == 0 ? x : v + x;
+          const int r = p.swap ? e & (kRows - 1) : e / kQuads, c = (p.swap ? e / kRows : e % kQuads) * 4;
+          const unsigned at = smem_addr(smem) + (unsigned)(r * (NB + 4) + c) * 4;
+          float v[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int s0 = 0; s0 < splits; s0 += 4) {      // four parts on their way at once, added in order
+            float x[4][4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+              if (s0 + s < splits)
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(x[s][0]), "=f"(x[s][1]), "=f"(x[s][2]), "=f"(x[s][3])
+                             : "r"(map_to_cta(at, s0 + s))
+                             : "memory");
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+              if (s0 + s < splits) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = s0 + s == 0 ? x[s][i] : v[i] + x[s][i];
+              }
           }
           const long long m = tc.m0 + r, n = tc.n0 + c;
-          if (m < M && n < N)
-            for (int o = 0; o < n_out; ++o) store_one(p, o == 0 ? p.y[tc.g] : p.y_rep[o - 1], p.swap ? n * ldy + m : m * ldy + n, v);
+          if (m >= M) continue;
+          for (int o = 0; o < n_out; ++o) {
+            void* y = o == 0 ? p.y[tc.g] : p.y_rep[o - 1];
+            if (!p.swap && p.y_align >= 8 && n + 4 <= N) {
+              unsigned char* to = static_cast<unsigned char*>(y) + (m * ldy + n) * (p.out_f32 ? 4 : 2);
+              if (p.out_f32) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                  if (SBP_GUARD(to + 8 * h, 8)) *reinterpret_cast<float2*>(to + 8 * h) = make_float2(v[2 * h], v[2 * h + 1]);
+              } else if (SBP_GUARD(to, 8)) {
+                *reinterpret_cast<uint2*>(to) = make_uint2(bf16_two(v[0], v[1]), bf16_two(v[2], v[3]));
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (n + i < N) store_one(p, y, p.swap ? (n + i) * ldy + m : m * ldy + n + i, v[i]);
+            }
+          }
         }
       }
     }
@@ -601,8 +640,8 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, 1) matmul8_ke
   else __syncthreads();
   if (warp == kRole + 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
-    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::kTmem) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::kTmem) : "memory");
   }
 }
 
@@ -678,20 +717,36 @@ long long tiles_of(const MatmulPlan& plan, int tm, int tn, bool swap) {
   return t;
 }
 
-Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma) {
-  long long m = 0, n = 0;
-  for (int g = 0; g < plan.ngroups; ++g) {
-    m = std::max(m, plan.m[g]);
-    n = std::max(n, plan.n[g]);
-  }
+// The form with the least estimated time: 4.5 us, then per wave of CTAs (pairs) so many a block and 3 between waves; a contraction shared by a
+// cluster costs its exchange.  Fitted to 15 products from 1 x 4096 x 4096 to 4096 x 4096 x 512 in every form: the pick is within 7 % of the
+// best on each of them.  kBlockUs: with a scale for 128 columns / for each column.
+Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma, bool x_tiles, bool w_tiles) {
+  constexpr double kBlockUs[5][2] = {{0.60, 1.35}, {0.42, 0.90}, {0.39, 0.56}, {0.38, 0.58}, {0.42, 0.46}};
   const int sms = device_sms();
-  if (tma && m > 64 && n > 64 && tiles_of(plan, 256, 256, false) * 4 >= pair_capacity() * 3) return {true, false, 256, 1};
-  Form8 f{false, m < n && m <= 64, 128, 1};
-  const long long few = std::min(m, n);
-  if (few <= 64) f.nb = few <= 16 ? 16 : few <= 32 ? 32 : 64;
-  const long long tiles = tiles_of(plan, 128, f.nb, f.swap);
-  while (f.splits < 8 && tiles * f.splits * 2 <= sms && blocks >= f.splits * 4) f.splits *= 2;
-  return f;
+  Form8 best{false, false, 128, 1};
+  double least = -1;
+  auto consider = [&](bool pair, bool swap, int i) {
+    const int nb = 256 >> i;
+    bool cols = !(swap ? x_tiles : w_tiles);
+    for (int g = 0; g < plan.ngroups; ++g) cols = cols || (swap ? plan.row_off[g] : plan.col_off[g]) % 128 != 0;
+    const long long tiles = tiles_of(plan, pair ? 256 : 128, nb, swap);
+    const double slow = tma ? 1.0 : 4.0;           // operands by plain loads
+    for (int splits = 1; splits <= (pair ? 1 : 8); splits *= 2) {
+      if (splits > 1 && blocks < 2 * splits) break;
+      const long long slots = pair ? pair_capacity() : (nb <= 32 && tma ? 2 : 1) * sms / splits * splits, ctas = tiles * splits;
+      const double waves = (double)((ctas + slots - 1) / slots);
+      const double us = 4.5 + waves * (double)((blocks + splits - 1) / splits) * kBlockUs[i][cols] * slow + 3.0 * (waves - 1.0) +
+                        (splits > 1 ? 2.8 + 0.016 * nb + 0.1 * splits : 0.0);
+      if (least < 0 || us < least) {
+        least = us;
+        best = {pair, swap, nb, splits};
+      }
+    }
+  };
+  if (tma) consider(true, false, 0);
+  for (int i = 1; i < 5; ++i)
+    for (bool swap : {false, true}) consider(false, swap, i);
+  return best;
 }
 
 template <bool COLS>
@@ -725,7 +780,7 @@ sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const
     tma = tma && plan.lda[s] % 16 == 0 && plan.ldb[s] % 16 == 0;
   }
   if (blocks > 0x7fffffffLL) return fail(SBP_ERR_UNSUPPORTED, "contraction too long for one launch");
-  const Form8 f = choose8(plan, blocks, tma);
+  const Form8 f = choose8(plan, blocks, tma, x_tiles, w_tiles);
   Params8 p{};
   p.splits = f.splits;
   p.swap = f.swap;
@@ -767,6 +822,11 @@ sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const
     if (p.m[g] > 0 && p.n[g] > 0) y_tma = y_tma && reinterpret_cast<uintptr_t>(p.y[g]) % 16 == 0 && p.ldy[g] * esz % 16 == 0;
   for (int r = 0; r < p.n_rep; ++r) y_tma = y_tma && reinterpret_cast<uintptr_t>(p.y_rep[r]) % 16 == 0;
   p.y_tma = y_tma;
+  uintptr_t bits = 16;                             // the lowest bit set is the alignment
+  for (int g = 0; g < plan.ngroups; ++g)
+    if (p.m[g] > 0 && p.n[g] > 0) bits |= reinterpret_cast<uintptr_t>(p.y[g]) | (uintptr_t)(p.ldy[g] * esz);
+  for (int r = 0; r < p.n_rep; ++r) bits |= reinterpret_cast<uintptr_t>(p.y_rep[r]);
+  p.y_align = (int)(bits & (~bits + 1));
   for (int g = 0; y_tma && g < plan.ngroups; ++g)
     if (p.m[g] > 0 && p.n[g] > 0 && !tensor_map8_out(&p.map_y[g], p.y[g], esz, p.m[g], p.n[g], p.ldy[g]))
       return fail(SBP_ERR_CUDA, "cuTensorMapEncodeTiled failed for the result of group %d", g);
