@@ -98,11 +98,6 @@ struct Eight<T, false> {
     for (int e = 0; e < 8; ++e) v_[e] = 0.f;
   }
   __device__ __forceinline__ void load(const T* p, int n, int step) {
-    if (n == 8 && SBP_GUARD(p, sizeof(T)) && SBP_GUARD(p + 7 * step, sizeof(T))) {      // (no test an element)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v_[e] = (float)p[e * step];
-      return;
-    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v_[e] = e < n && SBP_GUARD(p + e * step, sizeof(T)) ? (float)p[e * step] : 0.f;
   }
@@ -146,9 +141,6 @@ __device__ __forceinline__ void store8(float* p, const float* v, int n = 8, int 
       __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
       __stcs(reinterpret_cast<float4*>(p + 4), make_float4(v[4], v[5], v[6], v[7]));
     }
-  } else if (n == 8 && SBP_GUARD(p, 4) && SBP_GUARD(p + 7 * step, 4)) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e * step] = v[e];
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -160,9 +152,6 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* v, int n =
   if constexpr (VEC) {
     if (SBP_GUARD(p, 16))
       __stcs(reinterpret_cast<uint4*>(p), make_uint4(bf16_two(v[0], v[1]), bf16_two(v[2], v[3]), bf16_two(v[4], v[5]), bf16_two(v[6], v[7])));
-  } else if (n == 8 && SBP_GUARD(p, 2) && SBP_GUARD(p + 7 * step, 2)) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e * step] = __float2bfloat16_rn(v[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)

@@ -23,14 +23,16 @@ struct Jobs8 {
 };
 
 enum { kQuantize = 0, kGelu = 1, kGeluGrad = 2 };
-constexpr int kRowsAtOnce = 2;      // rows a team has in flight
+constexpr int rows_at_once(bool vec) { return vec ? 2 : 1; }      // rows a team has in flight
 
-// Blocks of 128 along the rows: a team of eight lanes a block, 16 elements a lane, two rows in flight.  (Eight elements a lane, 16 lanes a block: 13
+// Blocks of 128 along the rows: a team of eight lanes a block, 16 elements a lane, two rows in flight (one where elements are loaded one by one:
+// the code of two, fetched for a small tensor once, costs more than it hides).  (Eight elements a lane, 16 lanes a block: 13
 // instructions an element to quantise, 28 with GeLU, of which the conversions are 3 and GeLU 14; the rest is paid by lane and row.)
 template <typename TX, typename TY, int OP, bool VEC>
 __global__ void __launch_bounds__(256, VEC && sizeof(TX) == 2 ? 4 : 3) blocks8_row_kernel(const __grid_constant__ Jobs8 P) {
   SBP_PDL_RELEASE();
   SBP_PDL_WAIT();
+  constexpr int kRowsAtOnce = rows_at_once(VEC);
   const Job8& J = P.j[blockIdx.z];
   const int team = threadIdx.x >> 3, l = threadIdx.x & 7;
   const long long block = ((long long)blockIdx.y << P.per_row_log) + (team & ((1 << P.per_row_log) - 1));
@@ -72,9 +74,6 @@ __global__ void __launch_bounds__(256, VEC && sizeof(TX) == 2 ? 4 : 3) blocks8_r
         q[i][k] = make_uint2(0u, 0u);
         if constexpr (VEC) {
           if (in && n[k] > 0 && SBP_GUARD(src + 8 * k, 8)) q[i][k] = *reinterpret_cast<const uint2*>(src + 8 * k);
-        } else if (in && n[k] == 8 && SBP_GUARD(src + k * kNext, 1) && SBP_GUARD(src + k * kNext + 7 * kStep, 1)) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) (e < 4 ? q[i][k].x : q[i][k].y) |= (unsigned)src[k * kNext + e * kStep] << (8 * (e & 3));
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -152,10 +151,6 @@ __global__ void __launch_bounds__(256, VEC && sizeof(TX) == 2 ? 4 : 3) blocks8_r
       } else {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          if (n[k] == 8 && SBP_GUARD(dst + k * kNext, 1) && SBP_GUARD(dst + k * kNext + 7 * kStep, 1)) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dst[k * kNext + e * kStep] = (unsigned char)((e < 4 ? out[k].x : out[k].y) >> (8 * (e & 3)));
-          } else
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (e < n[k] && SBP_GUARD(dst + k * kNext + e * kStep, 1)) dst[k * kNext + e * kStep] = (unsigned char)((e < 4 ? out[k].x : out[k].y) >> (8 * (e & 3)));
@@ -422,7 +417,7 @@ sbp_status launch_rows(Jobs8& P, int n, cudaStream_t st) {
   P.wide = wide;
   P.per_row_log = 0;
   while (P.per_row_log < 5 && (1 << P.per_row_log) < blocks) ++P.per_row_log;
-  const long long rows_cta = (32 >> P.per_row_log) * kRowsAtOnce;
+  const long long rows_cta = (32 >> P.per_row_log) * rows_at_once(vec);
   const long long gx = (rows + rows_cta - 1) / rows_cta, gy = (blocks + (1 << P.per_row_log) - 1) >> P.per_row_log;
   if (gx > 0x7fffffffLL || gy > 65535) return fail(SBP_ERR_UNSUPPORTED, "tensor too large for one launch");
   const dim3 grid((unsigned)gx, (unsigned)gy, (unsigned)n);
