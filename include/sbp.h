@@ -571,8 +571,8 @@ sbp_status sbp_scales_shape(const sbp_tensor* values, uint32_t flags /* 0 or SBP
  * runs along its rows becomes one whose contraction is its last axis.  Signatures: S(i) or B (P: quantising is not linear). */
 sbp_status sbp_quantize8(const sbp_tensor* x, sbp_tensor* values, sbp_tensor* scales, uint32_t flags, void* cuda_stream);
 
-/* GeLU that keeps its input for the backward pass in 8 bits: y = z/2 (1 + erf(z / sqrt 2)), computed in fp32 (relative error below 2^-20),
- * F32 or BF16 like z, in one pass with values / scales = the blocks of z as sbp_quantize8(z) makes them.  All of one
+/* GeLU that keeps its input for the backward pass in 8 bits: y = z/2 (1 + erf(z / sqrt 2)), computed in fp32 (relative error below 2^-20 + z^2 2^-24,
+ * in the lower tail too; minus infinity gives 0), F32 or BF16, in one pass with values / scales = the blocks of z as sbp_quantize8(z) makes them.  All of one
  * shape and signature, S(i) or B. */
 sbp_status sbp_gelu_save8(const sbp_tensor* z, sbp_tensor* y, sbp_tensor* values, sbp_tensor* scales, void* cuda_stream);
 
@@ -586,9 +586,10 @@ sbp_status sbp_gelu_save8_backward(const sbp_tensor* values, const sbp_tensor* s
  *   y[m,n] = sum over blocks b of  x_scales[m,b] w_scales[n,b]  sum over k in b of  x[m,k] w[n,k]
  * with a row per element or per 128 (tiles) in either scales tensor, told apart by their first extent.  Signatures, fused results and
  * replicas as sbp_matmul (one-axis placements); y F32 or BF16.
- * A block's products are summed in fp32 on the tensor cores and its sum, scaled, is added to fp32 registers; few rows or columns are
- * cut along K over the CTAs of a cluster and joined in a fixed order.  Values whose base or leading dimension is not a multiple of 16
- * bytes are multiplied by a slower form of the kernel.  No workspace. */
+ * A block's products are summed in fp32 on the tensor cores; the sum times the product of its two scales (which has to lie in fp32's range) is
+ * added to fp32 registers.  Small results are cut along K over the CTAs of a cluster and joined in a fixed order: the same call gives the same bits.
+ * Values whose base or leading dimension is not a multiple of 16 bytes are multiplied by a slower form of the kernel (a leading dimension that is
+ * one, local_ld, avoids it).  w with a scale for every row instead of tiles takes about twice as long where the product is large.  No workspace. */
 sbp_status sbp_matmul8(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales, sbp_tensor* y,
                        void* cuda_stream);
 
