@@ -182,13 +182,15 @@ __device__ __forceinline__ unsigned long long pair_mul(unsigned long long a, uns
 // falls off as 1 / t: it is k times a polynomial in k = 1 / (1 + 0.304 t) fitted to it for the smallest relative error (6e-8, over t up to
 // 13.6; with its roundings 4e-7), so the tail keeps its digits until e underflows.
 // From t = 16 on e is zero: what is larger, infinities too, is taken for 16.  NaN stays NaN.
-// EXACT: z^2 is taken with what its rounding leaves, else its rounding is z^2 / 2 units in the last place of e (none for bf16 numbers).
+// FINITE: there are no infinities, and t is |z| itself (e is zero all the same).  EXACT: z^2 is taken with what its rounding leaves, else its rounding is z^2 / 2 units in the last place of e (none for bf16 numbers).
 // Cost: two special functions and some eleven instructions a number, for which erfcf and expf take about sixty.
-template <bool EXACT>
+template <bool EXACT, bool FINITE>
 __device__ __forceinline__ void tail_two(float a, float b, unsigned long long& t, unsigned long long& q, unsigned long long& e) {
-  float ta, tb;
-  asm("min.NaN.f32 %0, %1, 0f41800000;" : "=f"(ta) : "f"(fabsf(a)));
-  asm("min.NaN.f32 %0, %1, 0f41800000;" : "=f"(tb) : "f"(fabsf(b)));
+  float ta = fabsf(a), tb = fabsf(b);
+  if constexpr (!FINITE) {
+    asm("min.NaN.f32 %0, %0, 0f41800000;" : "+f"(ta));
+    asm("min.NaN.f32 %0, %0, 0f41800000;" : "+f"(tb));
+  }
   t = pair_of(ta, tb);
   const unsigned long long d = pair_fma(t, pair_of(0.30405593f), pair_of(1.0f));
   float ka, kb;
@@ -213,10 +215,10 @@ __device__ __forceinline__ void tail_two(float a, float b, unsigned long long& t
 }
 
 // GeLU(z) = z Phi(z) = max(z, 0) - |z| Phi(-|z|): below zero the tail alone, with its digits.  (Minus infinity gives 0.)
-template <bool EXACT>
+template <bool EXACT, bool FINITE>
 __device__ __forceinline__ void gelu_two(float& a, float& b) {
   unsigned long long t, q, e;
-  tail_two<EXACT>(a, b, t, q, e);
+  tail_two<EXACT, FINITE>(a, b, t, q, e);
   const unsigned long long y = pair_fma(t ^ 0x8000000080000000ull, q, pair_of(fmaxf(a, 0.f), fmaxf(b, 0.f)));
   a = pair_lo(y);
   b = pair_hi(y);
@@ -225,7 +227,7 @@ __device__ __forceinline__ void gelu_two(float& a, float& b) {
 // Its slope Phi(z) + z phi(z), phi(z) = e / sqrt(2 pi): with r = Phi(-t) - t phi(t), that is r below zero and 1 - r above.
 __device__ __forceinline__ void gelu_slope_two(float& a, float& b) {
   unsigned long long t, q, e;
-  tail_two<false>(a, b, t, q, e);
+  tail_two<false, false>(a, b, t, q, e);
   const unsigned long long r = pair_fma(pair_mul(t, e), pair_of(-0.39894228f), q);
   a = a < 0.f ? pair_lo(r) : 1.0f - pair_lo(r);
   b = b < 0.f ? pair_hi(r) : 1.0f - pair_hi(r);

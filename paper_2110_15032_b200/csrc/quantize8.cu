@@ -4,6 +4,8 @@
 // gradients.  Right behind it the instructions: 13 an element to quantise in a first form, 28 with GeLU (61 and 70 % of the issue slots).
 // Measured: bf16 [8192, 4096] quantised 17 us, 5.9 TB/s; [4096, 16384] by tiles, transposed 38 us, 5.3 TB/s; GeLU of [8192, 16384] 136 us, 5.0 TB/s, and its
 // gradient 135 us.
+#include <type_traits>
+
 #include "blocks8.h"
 
 namespace sbp {
@@ -94,11 +96,13 @@ __global__ void __launch_bounds__(256, VEC && sizeof(TX) == 2 ? 4 : 3) blocks8_r
         for (int e = 0; e < 8; e += 2) {
           float a, b;
           two_of_e4m3((e < 4 ? q[i][k].x : q[i][k].y) >> (8 * (e & 3)) & 0xffffu, a, b);
-          a *= s[i];
-          b *= s[i];
+          const unsigned long long z = pair_mul(pair_of(a, b), pair_of(s[i]));
+          a = pair_lo(z);
+          b = pair_hi(z);
           gelu_slope_two(a, b);
-          v[e] *= a;
-          v[e + 1] *= b;
+          const unsigned long long w = pair_mul(pair_of(v[e], v[e + 1]), pair_of(a, b));
+          v[e] = pair_lo(w);
+          v[e + 1] = pair_hi(w);
         }
         store8<VEC>(py + i * hop_y + k * kNext, v, n[k], kStep);
       }
@@ -125,22 +129,29 @@ __global__ void __launch_bounds__(256, VEC && sizeof(TX) == 2 ? 4 : 3) blocks8_r
       const unsigned sb = scale_bits(m);
       const float inv = __uint_as_float(kInvBits - sb);
       uint2 out[2];
+      auto convert = [&](auto fix_tag) {
+        constexpr bool FIX = decltype(fix_tag)::value;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float c[8];
-        x[i][k].get(c);
-        if (fix) {
+        for (int k = 0; k < 2; ++k) {
+          float c[8], w[8];
+          x[i][k].get(c);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) c[e] = inf_to_nan(c[e]);
+          for (int e = 0; e < 8; e += 2) {
+            const unsigned long long v = pair_mul(FIX ? pair_of(inf_to_nan(c[e]), inf_to_nan(c[e + 1])) : pair_of(c[e], c[e + 1]), pair_of(inv));
+            w[e] = pair_lo(v);
+            w[e + 1] = pair_hi(v);
+          }
+          out[k] = make_uint2(e4m3_four(w), e4m3_four(w + 4));
+          if constexpr (OP == kGelu) {
+            if (n[k] == 0) continue;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) gelu_two<sizeof(TX) == 4, !FIX && sizeof(TX) == 2>(c[e], c[e + 1]);
+            store8<VEC>(py + i * hop_y + k * kNext, c, n[k], kStep);
+          }
         }
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          const unsigned long long v = pair_mul(pair_of(c[e], c[e + 1]), pair_of(inv));
-          c[e] = pair_lo(v);
-          c[e + 1] = pair_hi(v);
-        }
-        out[k] = make_uint2(e4m3_four(c), e4m3_four(c + 4));
-      }
+      };
+      if (fix) convert(std::true_type{});
+      else convert(std::false_type{});
       unsigned char* dst = pq + i * hop_q;
       if constexpr (VEC) {
         if (P.wide) {
@@ -158,17 +169,6 @@ __global__ void __launch_bounds__(256, VEC && sizeof(TX) == 2 ? 4 : 3) blocks8_r
             if (e < n[k] && SBP_GUARD(dst + k * kNext + e * kStep, 1)) dst[k * kNext + e * kStep] = (unsigned char)((e < 4 ? out[k].x : out[k].y) >> (8 * (e & 3)));
       }
       if (l == 0 && SBP_GUARD(ps + i * hop_s, 4)) ps[i * hop_s] = __uint_as_float(sb);
-      if constexpr (OP == kGelu) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (n[k] == 0) continue;
-          float c[8];
-          x[i][k].get(c);
-#pragma unroll
-          for (int e = 0; e < 8; e += 2) gelu_two<sizeof(TX) == 4>(c[e], c[e + 1]);
-          store8<VEC>(py + i * hop_y + k * kNext, c, n[k], kStep);
-        }
-      }
     }
   }
 }
