@@ -120,7 +120,15 @@ __device__ __forceinline__ void tma_load_cta(unsigned dst, const CUtensorMap* ma
 // N accumulator columns of this warp's 32 rows
 template <int N>
 __device__ __forceinline__ void tmem_columns(unsigned taddr, float (&v)[N]) {
-  if constexpr (N == 32) {
+  if constexpr (N == 64) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+                   "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]),
+                   "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]), "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]),
+                   "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]), "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
+                 : "r"(taddr)
+                 : "memory");
+  } else if constexpr (N == 32) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
                  : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
                  : "r"(taddr)
@@ -136,6 +144,16 @@ __device__ __forceinline__ void tmem_columns(unsigned taddr, float (&v)[N]) {
                  : "r"(taddr)
                  : "memory");
   }
+}
+
+// 64 accumulator columns of 16 rows the way the matrix units lay out their results: of every eight columns lane t has 2 (t mod 4) and the next one, in rows t / 4
+// (v[4 g], v[4 g + 1]) and t / 4 + 8 (v[4 g + 2], v[4 g + 3]).
+__device__ __forceinline__ void tmem_fragments(unsigned taddr, float (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+                   "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+                 : "r"(taddr)
+                 : "memory");
 }
 
 template <bool PAIR, int NB, bool TMA>
@@ -222,6 +240,7 @@ __device__ __forceinline__ void store_one(const Params8& p, void* y, long long a
 template <bool PAIR, int NB, bool TMA, bool COLS>
 __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, NB, TMA>::kCtas) matmul8_kernel(const __grid_constant__ Params8 p) {
   using C = Shape8<PAIR, NB, TMA>;
+  constexpr bool kFragments = PAIR && COLS;        // a lane has 32 columns of four rows instead of 128 of one: a fourth of the columns' scales to load
   constexpr int kCols = C::kCols, kAccWarps = C::kAccWarps, kRole = kAccWarps;      // the first warp behind the accumulators
   constexpr int kTileM = PAIR ? 256 : 128;
   extern __shared__ unsigned char smem_raw[];
@@ -295,7 +314,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
         if (j == 0) {                              // the next blocks' scales
           ok = wait8(smem_addr(&bar_sc_full[ss]), s_round, abort_flag);
           if (!ok) break;
-          rs4 = *reinterpret_cast<const float4*>(scales + ss * C::kScales + row * kGroup);
+          if constexpr (!kFragments) rs4 = *reinterpret_cast<const float4*>(scales + ss * C::kScales + row * kGroup);
           if constexpr (!COLS) {
             const float4 cs = *reinterpret_cast<const float4*>(scales + ss * C::kScales + (kRows + part * kCols / 128) * kGroup);
             rs4 = make_float4(rs4.x * cs.x, rs4.y * cs.y, rs4.z * cs.z, rs4.w * cs.w);
@@ -304,23 +323,48 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
         const float rs = j == 0 ? rs4.x : j == 1 ? rs4.y : j == 2 ? rs4.z : rs4.w;
         const float* cs = scales + ss * C::kScales + kGroup * kRows + j * NB + part * kCols;
         {
-          constexpr int kStep = kCols < kLoad8 ? kCols : kLoad8;
+          constexpr int kStep = PAIR ? 64 : kCols < kLoad8 ? kCols : kLoad8;
           ok = wait8(smem_addr(&bar_acc_full[a]), a_round, abort_flag);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + part * kCols;
+          auto hand_back = [&]() {                 // the last columns are in registers: the accumulator goes back before they are added
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+              if constexpr (PAIR) mbar_arrive_cluster(acc_empty0 + a * 8);
+              else mbar_arrive(acc_empty0 + a * 8);
+            }
+          };
+          if constexpr (kFragments) {
+            const float* rsp = scales + ss * C::kScales + (q * 32 + (lane >> 2)) * kGroup + j;
+            const float r[4] = {rsp[0], rsp[8 * kGroup], rsp[16 * kGroup], rsp[24 * kGroup]};
+#pragma unroll
+            for (int b = 0; b < kCols; b += 64) {
+              float2 c[8];
+#pragma unroll
+              for (int g = 0; g < 8; ++g) c[g] = *reinterpret_cast<const float2*>(cs + b + g * 8 + (lane & 3) * 2);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float v[32];
+                tmem_fragments(at + b + ((unsigned)(h * 16) << 16), v);
+                if (b + 64 == kCols && h == 1) hand_back();
+                float* to = acc + (b / 64 * 2 + h) * 32;
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                  to[4 * g] = fmaf(v[4 * g] * c[g].x, r[2 * h], to[4 * g]);
+                  to[4 * g + 1] = fmaf(v[4 * g + 1] * c[g].y, r[2 * h], to[4 * g + 1]);
+                  to[4 * g + 2] = fmaf(v[4 * g + 2] * c[g].x, r[2 * h + 1], to[4 * g + 2]);
+                  to[4 * g + 3] = fmaf(v[4 * g + 3] * c[g].y, r[2 * h + 1], to[4 * g + 3]);
+                }
+              }
+            }
+          } else
 #pragma unroll
           for (int b = 0; b < kCols; b += kStep) {
             float v[kStep];
             tmem_columns(at + b, v);
-            if (b + kStep == kCols) {              // the last columns are in registers: the accumulator goes back before they are added
-              asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-              __syncwarp();
-              if (lane == 0) {
-                if constexpr (PAIR) mbar_arrive_cluster(acc_empty0 + a * 8);
-                else mbar_arrive(acc_empty0 + a * 8);
-              }
-            }
+            if (b + kStep == kCols) hand_back();
             float* to = acc + b;
             if constexpr (!COLS) {
 #pragma unroll
@@ -377,6 +421,18 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
             // the store before has been read out of the slab
             if (p.y_tma && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
             __syncwarp();
+            if constexpr (kFragments) {
+              constexpr int kGroups = kPiece / 8;  // of eight columns
+#pragma unroll
+              for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {      // rows lane / 4 + 8 r
+                  const int line = (lane >> 2) + 8 * r, from = s * kGroups + g;
+                  const float* f = acc + (from / 8 * 2 + r / 2) * 32 + from % 8 * 4 + r % 2 * 2;
+                  if constexpr (F32) *reinterpret_cast<float2*>(at_chunk(line, g * 2 + (lane >> 1 & 1)) + (lane & 1) * 8) = make_float2(f[0], f[1]);
+                  else *reinterpret_cast<unsigned*>(at_chunk(line, g) + (lane & 3) * 4) = bf16_two(f[0], f[1]);
+                }
+            } else {
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
               const float* f = acc + s * kPiece + c * kPer;
@@ -384,6 +440,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
               if constexpr (F32) o = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
               else o = make_uint4(bf16_two(f[0], f[1]), bf16_two(f[2], f[3]), bf16_two(f[4], f[5]), bf16_two(f[6], f[7]));
               *reinterpret_cast<uint4*>(at_chunk(lane, c)) = o;
+            }
             }
             if (kChunks == 8 && p.y_tma) {         // a whole slab
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
