@@ -15,12 +15,13 @@
 // Forms: a CTA pair with 256 x 256 tiles, persistent; single CTAs with 128 x NB tiles, cut along the contraction over a cluster where
 // there are few of them.  Few rows (columns): the 128 rows of the tile are the other operand's.
 //
-// Measured: 8192 x 4096 x 4096 (one scale for 128 columns) 139 us, 1.97 PFLOP/s, 1.2 times the bf16 GEMM rate; 2048^3 15.5 us; a weight of 16384 x 4096
-// under 16 rows 15.5 us.  Bound of the pair form: not the MMAs (512 of 1115 clocks a block) but the round from one block to the one that takes its
-// accumulator: products done, the warps woken, 128 columns read and added, the hand-back across the pair, the next products issued.  Without the additions
-// it takes 886 clocks, without the reads of tensor memory too 830.  Tried: accumulators of 128 and 160 columns, three and four of them (186 and 191 us: what a
-// warp pays a block, 400 clocks of waits, is paid more often), 16 accumulating warps (210 us), two loads of columns under way (142), waits that sleep
-// (197).  With a scale for each column 300 us: its 32 broadcast loads of shared memory a block and warp.
+// Measured: 8192 x 4096 x 4096 (one scale for 128 columns) 132 us, 2.09 PFLOP/s, 1.25 times the bf16 GEMM rate; 2048^3 15.5 us; a weight of 16384 x 4096
+// under 16 rows 15.5 us.  Bound of the pair form: not the MMAs (512 of 1060 clocks a block) but the round from one block to the one that takes its
+// accumulator: products done, the warps woken, 128 columns read and added, the hand-back across the pair, the next products issued.  A first form at 139 us
+// took 111 without the additions and 104 without the reads of tensor memory too.  Tried on it: accumulators of 128 and 160 columns, three and four of them (187 and
+// 191 us: what a warp pays a block, 400 clocks of waits, is paid more often), 16 accumulating warps (210), two loads of columns under way (142), additions one
+// by one instead of in pairs (136), waits that sleep (197).  With a scale for each column 218 us (300 with a row a lane, whose 32 broadcast loads a block take
+// shared memory's bandwidth).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -352,10 +353,12 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
                 float* to = acc + (b / 64 * 2 + h) * 32;
 #pragma unroll
                 for (int g = 0; g < 8; ++g) {
-                  to[4 * g] = fmaf(v[4 * g] * c[g].x, r[2 * h], to[4 * g]);
-                  to[4 * g + 1] = fmaf(v[4 * g + 1] * c[g].y, r[2 * h], to[4 * g + 1]);
-                  to[4 * g + 2] = fmaf(v[4 * g + 2] * c[g].x, r[2 * h + 1], to[4 * g + 2]);
-                  to[4 * g + 3] = fmaf(v[4 * g + 3] * c[g].y, r[2 * h + 1], to[4 * g + 3]);
+#pragma unroll
+                  for (int i = 0; i < 2; ++i) {
+                    const unsigned long long w = pair_fma(pair_mul(pair_of(v[4 * g + 2 * i], v[4 * g + 2 * i + 1]), pair_of(c[g].x, c[g].y)), pair_of(r[2 * h + i]), pair_of(to[4 * g + 2 * i], to[4 * g + 2 * i + 1]));
+                    to[4 * g + 2 * i] = pair_lo(w);
+                    to[4 * g + 2 * i + 1] = pair_hi(w);
+                  }
                 }
               }
             }
@@ -368,7 +371,11 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
             float* to = acc + b;
             if constexpr (!COLS) {
 #pragma unroll
-              for (int i = 0; i < kStep; ++i) to[i] = fmaf(v[i], rs, to[i]);
+              for (int i = 0; i < kStep; i += 2) {
+                const unsigned long long w = pair_fma(pair_of(v[i], v[i + 1]), pair_of(rs), pair_of(to[i], to[i + 1]));
+                to[i] = pair_lo(w);
+                to[i + 1] = pair_hi(w);
+              }
             } else {
 #pragma unroll
               for (int i = 0; i < kStep; i += 4) {
