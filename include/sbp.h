@@ -593,6 +593,13 @@ sbp_status sbp_gelu_save8_backward(const sbp_tensor* values, const sbp_tensor* s
 sbp_status sbp_matmul8(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales, sbp_tensor* y,
                        void* cuda_stream);
 
+/* Self-test of a wait that runs out inside such a product, safe to run anywhere: the same call, in which one of the eight warps (0..7) that
+ * keep the accumulators of a CTA acts as if its last wait had run out while the others finish.  For products whose contraction a
+ * cluster shares (few tiles, a long contraction), else SBP_ERR_UNSUPPORTED.  What y then holds is not defined; after the stream has
+ * drained sbp_check_device_errors() returns SBP_ERR_TIMEOUT once, and the device stays fully usable. */
+sbp_status sbp_selftest_matmul8_wait_timeout(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales,
+                                             sbp_tensor* y, int32_t warp, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

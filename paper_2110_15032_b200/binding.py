@@ -154,6 +154,7 @@ def load_library():
     lib.sbp_gelu_save8.argtypes = [T, T, T, T, C.c_void_p]
     lib.sbp_gelu_save8_backward.argtypes = [T, T, T, T, C.c_void_p]
     lib.sbp_matmul8.argtypes = [T, T, T, T, T, C.c_void_p]
+    lib.sbp_selftest_matmul8_wait_timeout.argtypes = [T, T, T, T, T, C.c_int32, C.c_void_p]
     _LIB = lib
     return lib
 
@@ -611,3 +612,9 @@ def sbp_matmul8(x: SbpTensor, x_scales: SbpTensor, w: SbpTensor, w_scales: SbpTe
     st = (_NATIVE or _native()).matmul8(x, x_scales, w, w_scales, y, stream)
     if st:
         _check(st)
+
+
+def sbp_selftest_matmul8_wait_timeout(x: SbpTensor, x_scales: SbpTensor, w: SbpTensor, w_scales: SbpTensor, y: SbpTensor, warp: int, stream=None) -> None:
+    """sbp_matmul8 in which accumulating warp `warp` acts as if its last wait had run out (see include/sbp.h)."""
+    a, b, c, d, e = (t._c() for t in (x, x_scales, w, w_scales, y))
+    _check(load_library().sbp_selftest_matmul8_wait_timeout(C.byref(a), C.byref(b), C.byref(c), C.byref(d), C.byref(e), int(warp), _stream_ptr(stream)))

@@ -69,6 +69,7 @@ struct Params8 {
   int y_align;                               // bytes that every row of the result (and of its replicas) is aligned to, 16 at most
   int out_f32, swap;                         // swap: rows of the tile are columns of the result
   int splits;                                // CTAs of a cluster that share a tile's contraction
+  int give_up;                               // self-test: this accumulating warp (1 to 8) acts as if its last wait had run out; 0: none
 };
 
 constexpr unsigned idesc8(int rows, int cols) { return (1u << 4) | ((unsigned)(cols >> 3) << 17) | ((unsigned)(rows >> 4) << 24); }
@@ -395,16 +396,25 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
           if (++ss == kScaleSlots) { ss = 0; s_round ^= 1; }
         }
       }
+      if (splits > 1) {                            // the partial tile, for the cluster to add up; the ring is done with
+        if (p.give_up == warp + 1) {
+          ok = false;
+          *abort_flag = 1;
+          atomicExch(&g_tc_timeout_flag, 1);
+        }
+        float* mine = reinterpret_cast<float*>(smem) + row * (NB + 4) + part * kCols;
+        // This barrier has no limit, so a warp whose wait ran out comes here too: others may have seen all their blocks.
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < kCols; i += 4) *reinterpret_cast<float4*>(mine + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+        break;                                     // (a cluster has one tile)
+      }
       if (!ok) break;
       const long long M = p.m[tc.g], N = p.n[tc.g], ldy = p.ldy[tc.g];
       const int n_out = (tc.g == 0 ? p.n_rep : 0) + 1;
       const long long row0 = tc.m0 + (int)rank * kRows, col0 = tc.n0 + part * kCols;
-      if (splits > 1) {                            // the partial tile, for the cluster to add up; the ring is done with
-        float* mine = reinterpret_cast<float*>(smem) + row * (NB + 4) + part * kCols;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < kCols; i += 4) *reinterpret_cast<float4*>(mine + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
-      } else if (p.swap) {                         // neighbouring lanes are neighbouring columns of the result
+      if (p.swap) {                         // neighbouring lanes are neighbouring columns of the result
         const long long n = row0 + row;
 #pragma unroll
         for (int i = 0; i < kCols; ++i) {
@@ -845,7 +855,7 @@ sbp_status launch8(const Params8& p, Form8 f, bool tma, cudaStream_t st) {
 }
 
 sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const sbp_tensor* w_scales, bool x_tiles, bool w_tiles,
-                       cudaStream_t st) {
+                       int give_up, cudaStream_t st) {
   bool tma = true;
   long long blocks = 0;
   int kblocks[SBP_MAX_K];
@@ -860,8 +870,10 @@ sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const
   }
   if (blocks > 0x7fffffffLL) return fail(SBP_ERR_UNSUPPORTED, "contraction too long for one launch");
   const Form8 f = choose8(plan, blocks, tma, x_tiles, w_tiles);
+  if (give_up && f.splits == 1) return fail(SBP_ERR_UNSUPPORTED, "no cluster shares this product's contraction");
   Params8 p{};
   p.splits = f.splits;
+  p.give_up = give_up;
   p.swap = f.swap;
   p.out_f32 = plan.out_dtype == SBP_F32;
   p.chain = plan.chain;
@@ -931,6 +943,23 @@ sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const
   return whole_blocks ? launch8<false>(p, f, tma, st) : launch8<true>(p, f, tma, st);
 }
 
+sbp_status matmul8(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales, sbp_tensor* y, int give_up,
+                   void* cuda_stream) {
+  MatmulPlan plan;
+  sbp_status st = build_matmul_plan(x, w, y, SBP_TRANS_W, true, true, &plan);
+  if (st != SBP_OK) return st;
+  bool x_tiles = false, w_tiles = false;
+  if ((st = check_blocks8(x, x_scales, "x", -1, true, &x_tiles)) != SBP_OK) return st;
+  if ((st = check_blocks8(w, w_scales, "w", -1, true, &w_tiles)) != SBP_OK) return st;
+  SBP_BOUNDS_RESET();
+  SBP_BOUNDS_TENSOR(x);
+  SBP_BOUNDS_TENSOR(x_scales);
+  SBP_BOUNDS_TENSOR(w);
+  SBP_BOUNDS_TENSOR(w_scales);
+  SBP_BOUNDS_TENSOR(y);
+  return run_matmul8(plan, x_scales, w_scales, x_tiles, w_tiles, give_up, static_cast<cudaStream_t>(cuda_stream));
+}
+
 }  // namespace
 
 sbp_status read_and_clear_matmul8_timeout(bool* timed_out) { return read_and_clear_timeout_flag(timed_out); }
@@ -944,19 +973,13 @@ extern "C" {
 sbp_status sbp_matmul8(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales, sbp_tensor* y,
                        void* cuda_stream) {
   SBP_RANGE("sbp_matmul8");
-  MatmulPlan plan;
-  sbp_status st = build_matmul_plan(x, w, y, SBP_TRANS_W, true, true, &plan);
-  if (st != SBP_OK) return st;
-  bool x_tiles = false, w_tiles = false;
-  if ((st = check_blocks8(x, x_scales, "x", -1, true, &x_tiles)) != SBP_OK) return st;
-  if ((st = check_blocks8(w, w_scales, "w", -1, true, &w_tiles)) != SBP_OK) return st;
-  SBP_BOUNDS_RESET();
-  SBP_BOUNDS_TENSOR(x);
-  SBP_BOUNDS_TENSOR(x_scales);
-  SBP_BOUNDS_TENSOR(w);
-  SBP_BOUNDS_TENSOR(w_scales);
-  SBP_BOUNDS_TENSOR(y);
-  return run_matmul8(plan, x_scales, w_scales, x_tiles, w_tiles, static_cast<cudaStream_t>(cuda_stream));
+  return matmul8(x, x_scales, w, w_scales, y, 0, cuda_stream);
+}
+
+sbp_status sbp_selftest_matmul8_wait_timeout(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales,
+                                             sbp_tensor* y, int32_t warp, void* cuda_stream) {
+  if (warp < 0 || warp > 7) return fail(SBP_ERR_INVALID_ARG, "warp must be in [0, 7]");
+  return matmul8(x, x_scales, w, w_scales, y, warp + 1, cuda_stream);
 }
 
 }  // extern "C"
