@@ -330,6 +330,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const unsigned at = tmem_base + ((unsigned)(q * 32) << 16) + a * C::kAccCols + part * kCols;
+          // (the two scales are multiplied by one another first: only their product has to lie in fp32's range)
           auto hand_back = [&]() {                 // the last columns are in registers: the accumulator goes back before they are added
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -356,7 +357,7 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
                 for (int g = 0; g < 8; ++g) {
 #pragma unroll
                   for (int i = 0; i < 2; ++i) {
-                    const unsigned long long w = pair_fma(pair_mul(pair_of(v[4 * g + 2 * i], v[4 * g + 2 * i + 1]), pair_of(c[g].x, c[g].y)), pair_of(r[2 * h + i]), pair_of(to[4 * g + 2 * i], to[4 * g + 2 * i + 1]));
+                    const unsigned long long w = pair_fma(pair_of(v[4 * g + 2 * i], v[4 * g + 2 * i + 1]), pair_mul(pair_of(c[g].x, c[g].y), pair_of(r[2 * h + i])), pair_of(to[4 * g + 2 * i], to[4 * g + 2 * i + 1]));
                     to[4 * g + 2 * i] = pair_lo(w);
                     to[4 * g + 2 * i + 1] = pair_hi(w);
                   }
@@ -381,10 +382,10 @@ __global__ void __launch_bounds__(Shape8<PAIR, NB, TMA>::kThreads, Shape8<PAIR, 
 #pragma unroll
               for (int i = 0; i < kStep; i += 4) {
                 const float4 s = *reinterpret_cast<const float4*>(cs + b + i);
-                to[i] = fmaf(v[i] * s.x, rs, to[i]);
-                to[i + 1] = fmaf(v[i + 1] * s.y, rs, to[i + 1]);
-                to[i + 2] = fmaf(v[i + 2] * s.z, rs, to[i + 2]);
-                to[i + 3] = fmaf(v[i + 3] * s.w, rs, to[i + 3]);
+                to[i] = fmaf(v[i], s.x * rs, to[i]);
+                to[i + 1] = fmaf(v[i + 1], s.y * rs, to[i + 1]);
+                to[i + 2] = fmaf(v[i + 2], s.z * rs, to[i + 2]);
+                to[i + 3] = fmaf(v[i + 3], s.w * rs, to[i + 3]);
               }
             }
           }
