@@ -532,8 +532,9 @@ sbp_status sbp_embedding_backward(const sbp_tensor* grad_out, const sbp_tensor* 
  *   beta   [n]       B, F32 or BF16; NULL: zeros
  *   y      as x in shape, signature and placement; F32 or BF16
  *   mean   [...]     x's shape without its last axis, x's signature, F32; NULL: not wanted (so rstd)
- * Sums are held in fp32, the squares are those of differences from the mean.  A row that holds a NaN or an infinity
- * is NaN; other rows are not affected.  n >= 1; no rows at all is fine.  eps >= 0 (a row of equal elements and eps 0: NaN).
+ * Sums are held in fp32, the squares are those of differences from the mean (squares that overflow leave rstd 0 and y beta).  A row that
+ * holds a NaN or an infinity is NaN; other rows are not affected.  n >= 1; no rows at all is fine.  eps >= 0.  A row of equal elements
+ * gives beta; where eps is 0 it has no deviation to divide by and is NaN.
  * A B tensor's replicas are each normalised by themselves, buffers that are shared by all of them once. */
 sbp_status sbp_layer_norm(const sbp_tensor* x, const sbp_tensor* gamma, const sbp_tensor* beta, sbp_tensor* y, sbp_tensor* mean,
                           sbp_tensor* rstd, float eps, void* cuda_stream);

@@ -172,6 +172,11 @@ __device__ __forceinline__ unsigned long long pair_fma(unsigned long long a, uns
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
   return v;
 }
+__device__ __forceinline__ unsigned long long pair_add(unsigned long long a, unsigned long long b) {
+  unsigned long long v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
 __device__ __forceinline__ unsigned long long pair_mul(unsigned long long a, unsigned long long b) {
   unsigned long long v;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));

@@ -7,6 +7,11 @@
 //
 // G threads share a row, each with NV times eight of its elements.  Rows too long for registers (over 16384, backward 8192) are read again for
 // each pass, out of L2.
+//
+// Mean and deviation: a first mean c from the row's sum, then the sum of d^2, d = x - c.  Where c is more than four deviations its own rounding shows beside them:
+// one more sum over the row gives f = sum d / n, the mean is c + f, the difference from it d - f and n times the variance sum d^2 - f sum d.  Of equal elements d
+// is a few units in the last place, at most 28 for rows in registers (32 additions in a thread, nine levels of a tree), so its sums are whole numbers of those
+// units and of their squares, below 28^2 2^14 < 2^24 and exact; f is d then, and the variance zero.
 #include <atomic>
 
 #include "blocks8.h"
@@ -66,29 +71,62 @@ struct Piece {
   }
 };
 
-// Sums over the G threads of a row; G over 32 is the whole block.  `turn` alternates between two buffers, so one barrier does.
-template <int G, int N>
-__device__ __forceinline__ void row_sums(float (&s)[N], float (*buf)[N][32], int& turn) {
+// Sums over the G threads of a row; G over 32 is the whole block.  `turn` alternates between two buffers, so one barrier does.  Of two sums each half of a
+// warp adds one, and every thread adds the warps' parts itself.
+template <int G, int N, typename T>
+__device__ __forceinline__ void row_sums(T (&s)[N], T (*buf)[N][32], int& turn) {
+  static_assert(N <= 2, "a half of the warp each");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  T v = s[0];
+  if constexpr (N == 2) {
+    const T other = lane & 16 ? s[0] : s[1];
+    v = lane & 16 ? s[1] : s[0];
+    v += __shfl_xor_sync(0xffffffffu, other, 16);
+  }
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) s[k] += __shfl_xor_sync(0xffffffffu, s[k], d);
+  for (int d = N == 2 ? 8 : 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
   if constexpr (G > 32) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) buf[turn][k][warp] = s[k];
-    }
+    if ((lane & (N == 2 ? 15 : 31)) == 0) buf[turn][lane >> 4][warp] = v;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      float v = lane < G / 32 ? buf[turn][k][lane] : 0.f;
+      T part[G / 32];
 #pragma unroll
-      for (int d = G / 64; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-      s[k] = __shfl_sync(0xffffffffu, v, 0);
+      for (int w = 0; w < G / 32; ++w) part[w] = buf[turn][k][w];
+#pragma unroll
+      for (int d = G / 64; d > 0; d >>= 1)
+#pragma unroll
+        for (int w = 0; w < d; ++w) part[w] += part[w + d];
+      s[k] = part[0];
     }
     turn ^= 1;
+  } else {
+    s[0] = v;
+    if constexpr (N == 2) {
+      s[0] = __shfl_sync(0xffffffffu, v, 0);
+      s[1] = __shfl_sync(0xffffffffu, v, 16);
+    }
   }
+}
+
+__device__ __forceinline__ void pairs_of(const float (&u)[8], unsigned long long (&v)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = pair_of(u[2 * e], u[2 * e + 1]);
+}
+
+// Is a first mean more than four times the deviation, by the sum of the squares of differences from it?  (NaN: no.  The mean of zeros is none.)
+__device__ __forceinline__ bool far_row(float c, float squares, float inv_n) { return squares * inv_n * 16.f <= c * c && c != 0.f; }
+
+// What the first mean is off by, given the sum of the differences: times the reciprocal of n, with one step of correction, right where the
+// quotient is a number of fp32.
+__device__ __forceinline__ float mean_off(float sum_d, float n, float inv_n) {
+  const float q = sum_d * inv_n;
+  return fmaf(fmaf(-q, n, sum_d), inv_n, q);
+}
+// 1 / deviation.  (Squares that overflow leave an infinite variance, as the multiply-add keeps it; NaN stays.)
+__device__ __forceinline__ float inverse_deviation(float squares, float f, float sum_d, float inv_n, float eps) {
+  const float var = fmaf(-f, sum_d, squares) * inv_n;
+  return 1.0f / sqrtf((var < 0.f ? 0.f : var) + eps);
 }
 
 constexpr int norm_threads(int g) { return g > 32 ? g : 256; }
@@ -150,18 +188,21 @@ constexpr int ring_bytes(int g, int nv, bool vec, bool backward) {
 template <typename TX, typename TY, int G, int NV, bool VEC>
 __global__ void __launch_bounds__(norm_threads(G), blocks_per_sm(G, NV, false)) norm_kernel(const __grid_constant__ NormParams P) {
   constexpr int kGroups = norm_threads(G) / G;
-  __shared__ float red[2][1][32];
+  __shared__ __align__(16) float red[2][1][32];
   SBP_PDL_RELEASE();
   SBP_PDL_WAIT();
   const NormJob& J = P.j[blockIdx.y];
   const int t = threadIdx.x % G;
-  const float inv_n = 1.0f / (float)P.cols;
-  float ga[NV][8], be[NV][8];
+  const float n = (float)P.cols, inv_n = 1.0f / n;
+  unsigned long long ga[NV][4], be[NV][4];         // (two numbers each, so that one instruction takes both)
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const Piece<G, VEC> at(i, t, P.cols);
-    vector8<VEC>(P.gamma, P.gamma_f32, P.gamma_whole, at.col, at.n, at.step, 1.f, ga[i]);
-    vector8<VEC>(P.beta, P.beta_f32, P.beta_whole, at.col, at.n, at.step, 0.f, be[i]);
+    float u[8];
+    vector8<VEC>(P.gamma, P.gamma_f32, P.gamma_whole, at.col, at.n, at.step, 1.f, u);
+    pairs_of(u, ga[i]);
+    vector8<VEC>(P.beta, P.beta_f32, P.beta_whole, at.col, at.n, at.step, 0.f, u);
+    pairs_of(u, be[i]);
   }
   int turn = 0;
   extern __shared__ __align__(16) unsigned char ring[];
@@ -179,52 +220,84 @@ __global__ void __launch_bounds__(norm_threads(G), blocks_per_sm(G, NV, false)) 
   }
   int slot = 0;
   for (; row < J.rows; row += stride) {
-    float v[NV][8];
-    float s[1] = {0.f};
-    if constexpr (VEC) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
-      take_row<TX, G, NV>(ring + slot * row_bytes<TX>(G, NV), v);
-      fetch(slot == 0 ? kRing - 1 : slot - 1, row + (kRing - 1) * stride);
-      slot = slot + 1 == kRing ? 0 : slot + 1;
-    } else {
+    unsigned long long v[NV][4];
+    {
+      float u[NV][8];
+      if constexpr (VEC) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
+        take_row<TX, G, NV>(ring + slot * row_bytes<TX>(G, NV), u);
+        fetch(slot == 0 ? kRing - 1 : slot - 1, row + (kRing - 1) * stride);
+        slot = slot + 1 == kRing ? 0 : slot + 1;
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const Piece<G, VEC> at(i, t, P.cols);
+          load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, u[i], at.n, at.step);      // (zeros behind the end)
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i) pairs_of(u[i], v[i]);
+    }
+    unsigned long long sum = 0ull;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (VEC && Piece<G, VEC>(i, t, P.cols).n == 0) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum = pair_add(sum, v[i][e]);
+    }
+    float s[1] = {pair_lo(sum) + pair_hi(sum)};
+    row_sums<G>(s, red, turn);
+    const float c = s[0] * inv_n;
+    sum = 0ull;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const Piece<G, VEC> at(i, t, P.cols);
+      if (VEC && at.n == 0) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[i][e] = pair_add(v[i][e], pair_of(-c));
+        if constexpr (!VEC) v[i][e] = pair_of(2 * e < at.n ? pair_lo(v[i][e]) : 0.f, 2 * e + 1 < at.n ? pair_hi(v[i][e]) : 0.f);
+        sum = pair_fma(v[i][e], v[i][e], sum);
+      }
+    }
+    s[0] = pair_lo(sum) + pair_hi(sum);
+    row_sums<G>(s, red, turn);
+    const float squares = s[0];
+    float f = 0.f;
+    s[0] = 0.f;
+    if (far_row(c, squares, inv_n)) {              // the same for all of the row's threads
+      sum = 0ull;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const Piece<G, VEC> at(i, t, P.cols);
-        if (at.n > 0) load8<VEC>(static_cast<const TX*>(J.x) + row * J.ldx + at.col, v[i], at.n, at.step);
+        if (VEC && Piece<G, VEC>(i, t, P.cols).n == 0) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum = pair_add(sum, v[i][e]);
       }
+      s[0] = pair_lo(sum) + pair_hi(sum);
+      row_sums<G>(s, red, turn);
+      f = mean_off(s[0], n, inv_n);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i][e] = pair_add(v[i][e], pair_of(-f));
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const Piece<G, VEC> at(i, t, P.cols);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < at.n) s[0] += v[i][e];
-    }
-    row_sums<G>(s, red, turn);
-    const float mean = s[0] * inv_n;
-    s[0] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const Piece<G, VEC> at(i, t, P.cols);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[i][e] -= mean;
-        if (e < at.n) s[0] = fmaf(v[i][e], v[i][e], s[0]);
-      }
-    }
-    row_sums<G>(s, red, turn);
-    const float rstd = 1.0f / sqrtf(fmaf(s[0], inv_n, P.eps));
+    const float rstd = inverse_deviation(squares, f, s[0], inv_n, P.eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const Piece<G, VEC> at(i, t, P.cols);
       if (at.n > 0) {
+        float u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * rstd, ga[i][e], be[i][e]);
-        store8<VEC>(static_cast<TY*>(J.out) + row * J.ldo + at.col, v[i], at.n, at.step);
+        for (int e = 0; e < 4; ++e) {
+          const unsigned long long y = pair_fma(pair_mul(v[i][e], pair_of(rstd)), ga[i][e], be[i][e]);
+          u[2 * e] = pair_lo(y);
+          u[2 * e + 1] = pair_hi(y);
+        }
+        store8<VEC>(static_cast<TY*>(J.out) + row * J.ldo + at.col, u, at.n, at.step);
       }
     }
     if (t == 0) {
-      if (J.mean && SBP_GUARD(J.mean + row, 4)) J.mean[row] = mean;
+      if (J.mean && SBP_GUARD(J.mean + row, 4)) J.mean[row] = c + f;
       if (J.rstd && SBP_GUARD(J.rstd + row, 4)) J.rstd[row] = rstd;
     }
   }
@@ -233,7 +306,7 @@ __global__ void __launch_bounds__(norm_threads(G), blocks_per_sm(G, NV, false)) 
 template <typename TX, typename TY, int G, int NV, bool VEC>
 __global__ void __launch_bounds__(norm_threads(G), blocks_per_sm(G, NV, true)) norm_grad_kernel(const __grid_constant__ NormParams P) {
   constexpr int kGroups = norm_threads(G) / G;
-  __shared__ float red[2][2][32];
+  __shared__ __align__(16) float red[2][2][32];
   SBP_PDL_RELEASE();
   SBP_PDL_WAIT();
   const NormJob& J = P.j[blockIdx.y];
@@ -354,34 +427,62 @@ __global__ void __launch_bounds__(norm_threads(G), blocks_per_sm(G, NV, true)) n
   }
 }
 
-// Rows longer than registers hold: a block a row, read once a pass.
+// Rows longer than registers hold: a block a row, read once a pass.  The first mean is that of a sum in 64 bits, of eight elements added as a tree (equal ones exactly) at a
+// time, so that equal elements are their mean whatever the row's length.
 constexpr int kWide = 512;
 template <typename TX, typename TY, bool VEC>
 __global__ void __launch_bounds__(kWide) norm_wide_kernel(const __grid_constant__ NormParams P) {
-  __shared__ float red[2][1][32];
+  __shared__ __align__(16) double red[2][1][32];
+  __shared__ __align__(16) float red2[2][1][32];
   SBP_PDL_RELEASE();
   SBP_PDL_WAIT();
   const NormJob& J = P.j[blockIdx.y];
   const int t = threadIdx.x, chunks = (int)((P.cols + 8 * kWide - 1) / (8 * kWide));
-  const float inv_n = 1.0f / (float)P.cols;
-  int turn = 0;
+  const float n = (float)P.cols, inv_n = 1.0f / n;
+  int turn = 0, turn2 = 0;
   for (long long row = blockIdx.x; row < J.rows; row += gridDim.x) {
     const TX* x = static_cast<const TX*>(J.x) + row * J.ldx;
-    float mean = 0.f, s[1], v[8];
-    for (int pass = 0; pass < 2; ++pass) {      // the sum, then the squares of what differs from the mean
-      s[0] = 0.f;
+    float v[8], q[1] = {0.f};
+    double s[1] = {0.0};
+    for (int i = 0; i < chunks; ++i) {
+      const Piece<kWide, VEC> at(i, t, P.cols);
+      if (at.n == 0) continue;
+      load8<VEC>(x + at.col, v, at.n, at.step);
+      if (at.n == 8) {
+        s[0] += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < at.n) s[0] += (double)v[e];
+      }
+    }
+    row_sums<kWide>(s, red, turn);
+    const float c = (float)(s[0] / (double)P.cols);
+    for (int i = 0; i < chunks; ++i) {
+      const Piece<kWide, VEC> at(i, t, P.cols);
+      if (at.n == 0) continue;
+      load8<VEC>(x + at.col, v, at.n, at.step);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < at.n) q[0] = fmaf(v[e] - c, v[e] - c, q[0]);
+    }
+    row_sums<kWide>(q, red2, turn2);
+    const float squares = q[0];
+    float f = 0.f;
+    q[0] = 0.f;
+    if (far_row(c, squares, inv_n)) {
       for (int i = 0; i < chunks; ++i) {
         const Piece<kWide, VEC> at(i, t, P.cols);
         if (at.n == 0) continue;
         load8<VEC>(x + at.col, v, at.n, at.step);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e < at.n) s[0] += pass ? (v[e] - mean) * (v[e] - mean) : v[e];
+          if (e < at.n) q[0] += v[e] - c;
       }
-      row_sums<kWide>(s, red, turn);
-      if (pass == 0) mean = s[0] * inv_n;
+      row_sums<kWide>(q, red2, turn2);
+      f = mean_off(q[0], n, inv_n);
     }
-    const float rstd = 1.0f / sqrtf(fmaf(s[0], inv_n, P.eps));
+    const float rstd = inverse_deviation(squares, f, q[0], inv_n, P.eps);
     for (int i = 0; i < chunks; ++i) {
       const Piece<kWide, VEC> at(i, t, P.cols);
       if (at.n == 0) continue;
@@ -389,12 +490,12 @@ __global__ void __launch_bounds__(kWide) norm_wide_kernel(const __grid_constant_
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (e < at.n)
-          v[e] = fmaf((v[e] - mean) * rstd, vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f),
+          v[e] = fmaf((v[e] - c - f) * rstd, vector_at(P.gamma, P.gamma_f32, at.col + e * at.step, 1.f),
                       vector_at(P.beta, P.beta_f32, at.col + e * at.step, 0.f));
       store8<VEC>(static_cast<TY*>(J.out) + row * J.ldo + at.col, v, at.n, at.step);
     }
     if (t == 0) {
-      if (J.mean && SBP_GUARD(J.mean + row, 4)) J.mean[row] = mean;
+      if (J.mean && SBP_GUARD(J.mean + row, 4)) J.mean[row] = c + f;
       if (J.rstd && SBP_GUARD(J.rstd + row, 4)) J.rstd[row] = rstd;
     }
   }
@@ -402,7 +503,7 @@ __global__ void __launch_bounds__(kWide) norm_wide_kernel(const __grid_constant_
 
 template <typename TX, typename TY, bool VEC>
 __global__ void __launch_bounds__(kWide) norm_grad_wide_kernel(const __grid_constant__ NormParams P) {
-  __shared__ float red[2][2][32];
+  __shared__ __align__(16) float red[2][2][32];
   SBP_PDL_RELEASE();
   SBP_PDL_WAIT();
   const NormJob& J = P.j[blockIdx.y];
