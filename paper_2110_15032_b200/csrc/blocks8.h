@@ -50,8 +50,8 @@ __device__ __forceinline__ unsigned finite_bits(float v) {
   const unsigned b = __float_as_uint(v) & 0x7fffffffu;
   return b < 0x7f800000u ? b : 0u;
 }
-// v, or NaN where v is infinite (the conversion would saturate it)
-__device__ __forceinline__ float inf_to_nan(float v) { return v + (v - v); }
+// v, its sign too where it is zero, or NaN where it is infinite (the conversion would saturate it)
+__device__ __forceinline__ float inf_to_nan(float v) { return v - (v - v); }
 
 // Eight elements of a row as they were loaded, so that loads may be ahead of their use at no more registers than the bytes need.
 // VEC: they follow one another, all are there and the first is 16-byte aligned; else the first `n` are there, `step` elements apart (so that
