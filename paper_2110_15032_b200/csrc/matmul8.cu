@@ -799,6 +799,11 @@ struct Form8 {
   int nb, splits;
 };
 
+// Which single forms there are.  Two are no product's choice (choose8): with one scale for 128 columns, 64 columns by the copy engine are dearer a
+// block and two to an SM fewer than 32; 16 columns by plain loads dearer a block than 32, more tiles, and 0.26 us less of exchange against
+// at least 0.32 us for the two blocks or more of every share.
+constexpr bool form_exists(int nb, bool tma, bool cols) { return cols || !(tma ? nb == 64 : nb == 16); }
+
 long long tiles_of(const MatmulPlan& plan, int tm, int tn, bool swap) {
   long long t = 0;
   for (int g = 0; g < plan.ngroups; ++g)
@@ -819,6 +824,7 @@ Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma, bool x_tiles, 
     const int nb = 256 >> i;
     bool cols = !(swap ? x_tiles : w_tiles);
     for (int g = 0; g < plan.ngroups; ++g) cols = cols || (swap ? plan.row_off[g] : plan.col_off[g]) % 128 != 0;
+    if (!form_exists(nb, tma, cols)) return;
     const long long tiles = tiles_of(plan, pair ? 256 : 128, nb, swap);
     const double slow = tma ? 1.0 : 4.0;           // operands by plain loads
     for (int splits = 1; splits <= (pair ? 1 : 8); splits *= 2) {
@@ -839,19 +845,25 @@ Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma, bool x_tiles, 
   return best;
 }
 
+template <int NB, bool TMA, bool COLS>
+sbp_status launch8_single(const Params8& p, int cluster, int ctas, cudaStream_t st) {
+  if constexpr (form_exists(NB, TMA, COLS)) return launch8_form<false, NB, TMA, COLS>(&p, cluster, ctas, st, nullptr);
+  else return fail(SBP_ERR_UNSUPPORTED, "no 8-bit matmul form of %d columns", NB);
+}
+
 template <bool COLS>
 sbp_status launch8(const Params8& p, Form8 f, bool tma, cudaStream_t st) {
-  if (f.pair) return launch8_form<true, 256, true, COLS>(&p, 2, 2 * std::min(p.total_tiles, pair_capacity()), st, nullptr);
   const int ctas = p.total_tiles * f.splits;
   switch (f.nb + (tma ? 0 : 1)) {
-    case 16: return launch8_form<false, 16, true, COLS>(&p, f.splits, ctas, st, nullptr);
-    case 17: return launch8_form<false, 16, false, COLS>(&p, f.splits, ctas, st, nullptr);
-    case 32: return launch8_form<false, 32, true, COLS>(&p, f.splits, ctas, st, nullptr);
-    case 33: return launch8_form<false, 32, false, COLS>(&p, f.splits, ctas, st, nullptr);
-    case 64: return launch8_form<false, 64, true, COLS>(&p, f.splits, ctas, st, nullptr);
-    case 65: return launch8_form<false, 64, false, COLS>(&p, f.splits, ctas, st, nullptr);
-    case 128: return launch8_form<false, 128, true, COLS>(&p, f.splits, ctas, st, nullptr);
-    default: return launch8_form<false, 128, false, COLS>(&p, f.splits, ctas, st, nullptr);
+    case 256: return launch8_form<true, 256, true, COLS>(&p, 2, 2 * std::min(p.total_tiles, pair_capacity()), st, nullptr);
+    case 16: return launch8_single<16, true, COLS>(p, f.splits, ctas, st);
+    case 17: return launch8_single<16, false, COLS>(p, f.splits, ctas, st);
+    case 32: return launch8_single<32, true, COLS>(p, f.splits, ctas, st);
+    case 33: return launch8_single<32, false, COLS>(p, f.splits, ctas, st);
+    case 64: return launch8_single<64, true, COLS>(p, f.splits, ctas, st);
+    case 65: return launch8_single<64, false, COLS>(p, f.splits, ctas, st);
+    case 128: return launch8_single<128, true, COLS>(p, f.splits, ctas, st);
+    default: return launch8_single<128, false, COLS>(p, f.splits, ctas, st);
   }
 }
 
