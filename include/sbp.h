@@ -594,6 +594,16 @@ sbp_status sbp_gelu_save8_backward(const sbp_tensor* values, const sbp_tensor* s
 sbp_status sbp_matmul8(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales, sbp_tensor* y,
                        void* cuda_stream);
 
+/* A product runs on tiles of 256 x 256 (a pair of CTAs) or of 128 rows and 128, 64, 32 or 16 columns, whose contraction 1, 2, 4 or 8 CTAs share and
+ * whose operands may be exchanged (then the tile's rows are columns of y); the library picks by estimated time.  sbp_matmul8_set_form overrides
+ * the choice for tests and measurements (process-wide, not a tuning knob): columns 0 = the library chooses; 256 goes with splits 1, not
+ * exchanged.  A product that cannot run the forced form runs it with fewer splits (each share has two blocks at least) or, where that form does not
+ * exist for it (256 columns of operands that are not read by the copy engine; one scale for 128 columns in tiles of 64 by the copy engine
+ * or of 16 without it), the library's choice.  sbp_matmul8_form_launches reports the launches of a form since the library was loaded:
+ * copy_engine: operands in whole 16-byte pieces; scale_each: a scale for each column of the tile, not one for 128. */
+sbp_status sbp_matmul8_set_form(int32_t columns, int32_t splits, int32_t exchanged);
+uint64_t sbp_matmul8_form_launches(int32_t columns, int32_t splits, int32_t exchanged, int32_t copy_engine, int32_t scale_each);
+
 /* Self-test of a wait that runs out inside such a product, safe to run anywhere: the same call, in which one of the eight warps (0..7) that
  * keep the accumulators of a CTA acts as if its last wait had run out while the others finish.  For products whose contraction a
  * cluster shares (few tiles, a long contraction), else SBP_ERR_UNSUPPORTED.  What y then holds is not defined; after the stream has

@@ -13,5 +13,5 @@ from .binding import (  # noqa: F401
     sbp_matmul_infer, sbp_matmul_workspace_bytes_preferred, sbp_matmul_softmax_xent, sbp_matmul_softmax_xent_backward, sbp_matmul_softmax_xent_workspace_bytes, sbp_matmul_workspace_bytes, sbp_selftest_wait_timeout, sbp_softmax_xent,
     sbp_softmax_xent_backward, sbp_transfer_cost, sbp_softmax_xent_static, sbp_softmax_xent_workspace_bytes, SBP_EPILOGUE_GELU, SBP_TRANS_X, SBP_TRANS_W, SBP_QUANT_TILES,
     sbp_layer_norm, sbp_layer_norm_backward, sbp_layer_norm_backward_workspace_bytes, sbp_scales_shape, sbp_quantize8, sbp_gelu_save8,
-    sbp_gelu_save8_backward, sbp_matmul8, sbp_selftest_matmul8_wait_timeout,
+    sbp_gelu_save8_backward, sbp_matmul8, sbp_matmul8_set_form, sbp_matmul8_form_launches, sbp_selftest_matmul8_wait_timeout,
 )

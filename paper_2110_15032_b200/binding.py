@@ -154,6 +154,9 @@ def load_library():
     lib.sbp_gelu_save8.argtypes = [T, T, T, T, C.c_void_p]
     lib.sbp_gelu_save8_backward.argtypes = [T, T, T, T, C.c_void_p]
     lib.sbp_matmul8.argtypes = [T, T, T, T, T, C.c_void_p]
+    lib.sbp_matmul8_set_form.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+    lib.sbp_matmul8_form_launches.argtypes = [C.c_int32] * 5
+    lib.sbp_matmul8_form_launches.restype = C.c_uint64
     lib.sbp_selftest_matmul8_wait_timeout.argtypes = [T, T, T, T, T, C.c_int32, C.c_void_p]
     _LIB = lib
     return lib
@@ -612,6 +615,16 @@ def sbp_matmul8(x: SbpTensor, x_scales: SbpTensor, w: SbpTensor, w_scales: SbpTe
     st = (_NATIVE or _native()).matmul8(x, x_scales, w, w_scales, y, stream)
     if st:
         _check(st)
+
+
+def sbp_matmul8_set_form(columns: int = 0, splits: int = 1, exchanged: bool = False) -> None:
+    """Test and measurement override of the form that 8-bit products run in (columns 0: the library chooses)."""
+    _check(load_library().sbp_matmul8_set_form(int(columns), int(splits), 1 if exchanged else 0))
+
+
+def sbp_matmul8_form_launches(columns: int, splits: int, exchanged: bool, copy_engine: bool, scale_each: bool) -> int:
+    """Launches of one form of the 8-bit product since the library was loaded."""
+    return int(load_library().sbp_matmul8_form_launches(int(columns), int(splits), int(exchanged), int(copy_engine), int(scale_each)))
 
 
 def sbp_selftest_matmul8_wait_timeout(x: SbpTensor, x_scales: SbpTensor, w: SbpTensor, w_scales: SbpTensor, y: SbpTensor, warp: int, stream=None) -> None:

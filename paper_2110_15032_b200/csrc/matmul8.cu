@@ -804,6 +804,13 @@ struct Form8 {
 // at least 0.32 us for the two blocks or more of every share.
 constexpr bool form_exists(int nb, bool tma, bool cols) { return cols || !(tma ? nb == 64 : nb == 16); }
 
+// What sbp_matmul8_set_form asks for: columns | splits << 16 | swap << 24; 0: the library chooses.
+std::atomic<int> g_form8{0};
+// Launches by columns (256 >> index), log2 of the CTAs that share a contraction, swap, copy engine, scale for each column.
+std::atomic<unsigned long long> g_launches8[5][4][2][2][2];
+int form_index(int nb) { return nb == 256 ? 0 : nb == 128 ? 1 : nb == 64 ? 2 : nb == 32 ? 3 : nb == 16 ? 4 : -1; }
+int split_index(int splits) { return splits == 1 ? 0 : splits == 2 ? 1 : splits == 4 ? 2 : splits == 8 ? 3 : -1; }
+
 long long tiles_of(const MatmulPlan& plan, int tm, int tn, bool swap) {
   long long t = 0;
   for (int g = 0; g < plan.ngroups; ++g)
@@ -820,10 +827,19 @@ Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma, bool x_tiles, 
   const int sms = device_sms();
   Form8 best{false, false, 128, 1};
   double least = -1;
-  auto consider = [&](bool pair, bool swap, int i) {
-    const int nb = 256 >> i;
+  auto scale_each = [&](bool swap) {
     bool cols = !(swap ? x_tiles : w_tiles);
     for (int g = 0; g < plan.ngroups; ++g) cols = cols || (swap ? plan.row_off[g] : plan.col_off[g]) % 128 != 0;
+    return cols;
+  };
+  if (const int want = g_form8.load(std::memory_order_relaxed)) {
+    Form8 f{(want & 0xffff) == 256, (want >> 24) != 0, want & 0xffff, (want >> 16) & 0xff};
+    while (f.splits > 1 && blocks < 2 * f.splits) f.splits /= 2;
+    if (f.pair ? tma : form_exists(f.nb, tma, scale_each(f.swap))) return f;
+  }
+  auto consider = [&](bool pair, bool swap, int i) {
+    const int nb = 256 >> i;
+    const bool cols = scale_each(swap);
     if (!form_exists(nb, tma, cols)) return;
     const long long tiles = tiles_of(plan, pair ? 256 : 128, nb, swap);
     const double slow = tma ? 1.0 : 4.0;           // operands by plain loads
@@ -854,17 +870,20 @@ sbp_status launch8_single(const Params8& p, int cluster, int ctas, cudaStream_t 
 template <bool COLS>
 sbp_status launch8(const Params8& p, Form8 f, bool tma, cudaStream_t st) {
   const int ctas = p.total_tiles * f.splits;
+  sbp_status s;
   switch (f.nb + (tma ? 0 : 1)) {
-    case 256: return launch8_form<true, 256, true, COLS>(&p, 2, 2 * std::min(p.total_tiles, pair_capacity()), st, nullptr);
-    case 16: return launch8_single<16, true, COLS>(p, f.splits, ctas, st);
-    case 17: return launch8_single<16, false, COLS>(p, f.splits, ctas, st);
-    case 32: return launch8_single<32, true, COLS>(p, f.splits, ctas, st);
-    case 33: return launch8_single<32, false, COLS>(p, f.splits, ctas, st);
-    case 64: return launch8_single<64, true, COLS>(p, f.splits, ctas, st);
-    case 65: return launch8_single<64, false, COLS>(p, f.splits, ctas, st);
-    case 128: return launch8_single<128, true, COLS>(p, f.splits, ctas, st);
-    default: return launch8_single<128, false, COLS>(p, f.splits, ctas, st);
+    case 256: s = launch8_form<true, 256, true, COLS>(&p, 2, 2 * std::min(p.total_tiles, pair_capacity()), st, nullptr); break;
+    case 16: s = launch8_single<16, true, COLS>(p, f.splits, ctas, st); break;
+    case 17: s = launch8_single<16, false, COLS>(p, f.splits, ctas, st); break;
+    case 32: s = launch8_single<32, true, COLS>(p, f.splits, ctas, st); break;
+    case 33: s = launch8_single<32, false, COLS>(p, f.splits, ctas, st); break;
+    case 64: s = launch8_single<64, true, COLS>(p, f.splits, ctas, st); break;
+    case 65: s = launch8_single<64, false, COLS>(p, f.splits, ctas, st); break;
+    case 128: s = launch8_single<128, true, COLS>(p, f.splits, ctas, st); break;
+    default: s = launch8_single<128, false, COLS>(p, f.splits, ctas, st); break;
   }
+  if (s == SBP_OK) g_launches8[form_index(f.nb)][split_index(f.splits)][f.swap][tma][COLS].fetch_add(1, std::memory_order_relaxed);
+  return s;
 }
 
 sbp_status run_matmul8(const MatmulPlan& plan, const sbp_tensor* x_scales, const sbp_tensor* w_scales, bool x_tiles, bool w_tiles,
@@ -987,6 +1006,19 @@ sbp_status sbp_matmul8(const sbp_tensor* x, const sbp_tensor* x_scales, const sb
                        void* cuda_stream) {
   SBP_RANGE("sbp_matmul8");
   return matmul8(x, x_scales, w, w_scales, y, 0, cuda_stream);
+}
+
+sbp_status sbp_matmul8_set_form(int32_t columns, int32_t splits, int32_t exchanged) {
+  const bool pair = columns == 256;
+  if (columns != 0 && (form_index(columns) < 0 || split_index(splits) < 0 || (pair && (splits != 1 || exchanged))))
+    return fail(SBP_ERR_INVALID_ARG, "no form of %d columns with %d splits", columns, splits);
+  g_form8.store(columns == 0 ? 0 : columns | splits << 16 | (exchanged ? 1 << 24 : 0), std::memory_order_relaxed);
+  return SBP_OK;
+}
+
+uint64_t sbp_matmul8_form_launches(int32_t columns, int32_t splits, int32_t exchanged, int32_t copy_engine, int32_t scale_each) {
+  const int c = form_index(columns), s = split_index(splits);
+  return c < 0 || s < 0 ? 0 : g_launches8[c][s][exchanged != 0][copy_engine != 0][scale_each != 0].load(std::memory_order_relaxed);
 }
 
 sbp_status sbp_selftest_matmul8_wait_timeout(const sbp_tensor* x, const sbp_tensor* x_scales, const sbp_tensor* w, const sbp_tensor* w_scales,
