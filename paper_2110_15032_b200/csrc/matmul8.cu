@@ -823,7 +823,7 @@ long long tiles_of(const MatmulPlan& plan, int tm, int tn, bool swap) {
 // cluster costs its exchange.  Fitted to 15 products from 1 x 4096 x 4096 to 4096 x 4096 x 512 in every form; over those and 14 drawn
 // ones the pick is 4 % off the best form on the average, 44, 26 and 23 % on the worst three.  kBlockUs: with a scale for 128 columns / for each column.
 Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma, bool x_tiles, bool w_tiles) {
-  constexpr double kBlockUs[5][2] = {{0.60, 1.35}, {0.42, 0.90}, {0.39, 0.56}, {0.38, 0.58}, {0.42, 0.46}};
+  constexpr double kBlockUs[5][2] = {{0.60, 0.97}, {0.42, 0.90}, {0.39, 0.56}, {0.38, 0.58}, {0.42, 0.46}};
   const int sms = device_sms();
   Form8 best{false, false, 128, 1};
   double least = -1;
