@@ -778,18 +778,49 @@ sbp_status launch8_form(const Params8* p, int cluster, int ctas, cudaStream_t st
   return SBP_OK;
 }
 
-// CTA pairs that the device holds at once, asked once a device.
-int pair_capacity() {
-  static std::atomic<int> known[64];
+int split_index(int splits) { return splits == 1 ? 0 : splits == 2 ? 1 : splits == 4 ? 2 : splits == 8 ? 3 : -1; }
+
+// Never launched: how many clusters the device holds is asked of it, with a form's threads and shared memory.  (Of a kernel that allocates tensor memory
+// the runtime says that an SM holds one CTA, also where it runs two.)
+__global__ void __launch_bounds__(512) seats_kernel() {}
+
+// Clusters that the device holds at once, asked once a device: of CTA pairs with 256 columns, of `splits` CTAs that take an SM each, or of those of which an
+// SM holds two.  148 SMs have room for 37 clusters of four and 18 of eight by their number, for 33 and 15 by where they lie; of two to an SM for 71 and 33.
+// Products of 33 and 34, 15 and 16, 71 and 72, 33 and 34 such clusters: 21.6 and 38.9, 19.1 and 34.5, 19.1 and 29.2, 16.3 and 24.4 us.
+enum { kPairs = 0, kAlone = 1, kTwo = 2 };
+sbp_status ask_clusters(int kind, int splits, int* n) {
+  if (kind == kPairs) return launch8_form<true, 256, true, false>(nullptr, 2, 0, nullptr, n);
+  constexpr int kStatic = 1024;                    // barriers, and what the launch itself takes
+  const int smem = (kind == kTwo ? Shape8<false, 32, true>::kSmem : Shape8<false, 128, true>::kSmem) + kStatic;
+  SBP_CUDA_TRY(cudaFuncSetAttribute(seats_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(device_sms() / splits * splits));
+  cfg.blockDim = dim3(Shape8<false, 32, true>::kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)splits;
+  attr.val.clusterDim.y = 1;
+  attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  SBP_CUDA_TRY(cudaOccupancyMaxActiveClusters(n, seats_kernel, &cfg));
+  return SBP_OK;
+}
+int cluster_capacity(int kind, int splits) {
+  static std::atomic<int> known[64][3][4];
+  const int by_number = device_sms() * (kind == kTwo ? 2 : 1) / (kind == kPairs ? 2 : splits);
+  if (kind != kPairs && splits == 1) return by_number;
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return device_sms() / 2;
-  int n = known[dev].load(std::memory_order_relaxed);
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return by_number;
+  std::atomic<int>& slot = known[dev][kind][split_index(splits)];
+  int n = slot.load(std::memory_order_relaxed);
   if (n == 0) {
-    if (launch8_form<true, 256, true, false>(nullptr, 2, 0, nullptr, &n) != SBP_OK || n < 1) {
+    if (ask_clusters(kind, splits, &n) != SBP_OK || n < 1) {
       cudaGetLastError();
-      n = device_sms() / 2;
+      n = by_number;
     }
-    known[dev].store(n, std::memory_order_relaxed);
+    slot.store(n, std::memory_order_relaxed);
   }
   return n;
 }
@@ -809,7 +840,6 @@ std::atomic<int> g_form8{0};
 // Launches by columns (256 >> index), log2 of the CTAs that share a contraction, swap, copy engine, scale for each column.
 std::atomic<unsigned long long> g_launches8[5][4][2][2][2];
 int form_index(int nb) { return nb == 256 ? 0 : nb == 128 ? 1 : nb == 64 ? 2 : nb == 32 ? 3 : nb == 16 ? 4 : -1; }
-int split_index(int splits) { return splits == 1 ? 0 : splits == 2 ? 1 : splits == 4 ? 2 : splits == 8 ? 3 : -1; }
 
 long long tiles_of(const MatmulPlan& plan, int tm, int tn, bool swap) {
   long long t = 0;
@@ -819,12 +849,13 @@ long long tiles_of(const MatmulPlan& plan, int tm, int tn, bool swap) {
   return t;
 }
 
-// The form with the least estimated time: 4.5 us, then per wave of CTAs (pairs) so many a block and 3 between waves; a contraction shared by a
-// cluster costs its exchange.  Fitted to 15 products from 1 x 4096 x 4096 to 4096 x 4096 x 512 in every form; over those and 14 drawn
-// ones the pick is 4 % off the best form on the average, 44, 26 and 23 % on the worst three.  kBlockUs: with a scale for 128 columns / for each column.
+// The form with the least estimated time: 4.5 us, then per wave of clusters (pairs) so many a block and 3 between waves; a contraction shared by a
+// cluster costs its exchange.  kBlockUs: with a scale for 128 columns / for each column.
+// Of 68 products from 1 x 4096 x 4096 to 4096 x 16384 x 1024, 40 of them drawn, with both kinds of scales the pick is 5 % off the best form on the average; the
+// worst are 9 x 4576 x 736 (12.5 for 7.5 us), 28 x 8288 x 592 (10.8 for 7.2) and 4 x 6128 x 224 (8.2 for 5.6), products of a few blocks and many
+// CTAs, whose start the estimate does not count; 64 x 4096 x 4096 is 15.0 for 12.2.
 Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma, bool x_tiles, bool w_tiles) {
   constexpr double kBlockUs[5][2] = {{0.60, 0.97}, {0.42, 0.90}, {0.39, 0.56}, {0.38, 0.58}, {0.42, 0.46}};
-  const int sms = device_sms();
   Form8 best{false, false, 128, 1};
   double least = -1;
   auto scale_each = [&](bool swap) {
@@ -845,8 +876,8 @@ Form8 choose8(const MatmulPlan& plan, long long blocks, bool tma, bool x_tiles, 
     const double slow = tma ? 1.0 : 4.0;           // operands by plain loads
     for (int splits = 1; splits <= (pair ? 1 : 8); splits *= 2) {
       if (splits > 1 && blocks < 2 * splits) break;
-      const long long slots = pair ? pair_capacity() : (nb <= 32 && tma ? 2 : 1) * sms / splits * splits, ctas = tiles * splits;
-      const double waves = (double)((ctas + slots - 1) / slots);
+      const long long held = cluster_capacity(pair ? kPairs : nb <= 32 && tma ? kTwo : kAlone, splits);
+      const double waves = (double)((tiles + held - 1) / held);
       const double us = 4.5 + waves * (double)((blocks + splits - 1) / splits) * kBlockUs[i][cols] * slow + 3.0 * (waves - 1.0) +
                         (splits > 1 ? 2.8 + 0.016 * nb + 0.1 * splits : 0.0);
       if (least < 0 || us < least) {
@@ -872,7 +903,7 @@ sbp_status launch8(const Params8& p, Form8 f, bool tma, cudaStream_t st) {
   const int ctas = p.total_tiles * f.splits;
   sbp_status s;
   switch (f.nb + (tma ? 0 : 1)) {
-    case 256: s = launch8_form<true, 256, true, COLS>(&p, 2, 2 * std::min(p.total_tiles, pair_capacity()), st, nullptr); break;
+    case 256: s = launch8_form<true, 256, true, COLS>(&p, 2, 2 * std::min(p.total_tiles, cluster_capacity(kPairs, 1)), st, nullptr); break;
     case 16: s = launch8_single<16, true, COLS>(p, f.splits, ctas, st); break;
     case 17: s = launch8_single<16, false, COLS>(p, f.splits, ctas, st); break;
     case 32: s = launch8_single<32, true, COLS>(p, f.splits, ctas, st); break;
