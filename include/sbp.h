@@ -60,7 +60,8 @@ typedef enum {
   SBP_I64 = 2,
   SBP_E4M3 = 3 /* 8-bit floating point: 4 exponent bits, 3 mantissa bits, largest 448, no infinity.  Taken by
                   sbp_local_shape and by the entry points on 8-bit blocks; every other one answers
-                  SBP_ERR_DTYPE.  (To box such a tensor, describe pairs of values as one BF16.) */
+                  SBP_ERR_DTYPE.  (To box such a tensor, describe pairs of values as one BF16: the
+                  extent of its last axis, and of every part where that axis is split, has to be even.) */
 } sbp_dtype;
 
 typedef enum {
@@ -533,8 +534,9 @@ sbp_status sbp_embedding_backward(const sbp_tensor* grad_out, const sbp_tensor* 
  *   y      as x in shape, signature and placement; F32 or BF16
  *   mean   [...]     x's shape without its last axis, x's signature, F32; NULL: not wanted (so rstd)
  * Sums are held in fp32, the squares are those of differences from the mean (squares that overflow leave rstd 0 and y beta).  A row that
- * holds a NaN or an infinity is NaN; other rows are not affected.  n >= 1; no rows at all is fine.  eps >= 0.  A row of equal elements
- * gives beta; where eps is 0 it has no deviation to divide by and is NaN.
+ * holds a NaN or an infinity, or whose sum overflows, is NaN; other rows are not affected.  n >= 1; no rows at all is fine.  eps >= 0.  A
+ * row of equal elements gives beta; where eps is 0 it has no deviation to divide by and is NaN (of elements below 2^-50, the squares of
+ * whose last places leave fp32's range, NaN or beta).
  * A B tensor's replicas are each normalised by themselves, buffers that are shared by all of them once. */
 sbp_status sbp_layer_norm(const sbp_tensor* x, const sbp_tensor* gamma, const sbp_tensor* beta, sbp_tensor* y, sbp_tensor* mean,
                           sbp_tensor* rstd, float eps, void* cuda_stream);
@@ -573,8 +575,8 @@ sbp_status sbp_scales_shape(const sbp_tensor* values, uint32_t flags /* 0 or SBP
 sbp_status sbp_quantize8(const sbp_tensor* x, sbp_tensor* values, sbp_tensor* scales, uint32_t flags, void* cuda_stream);
 
 /* GeLU that keeps its input for the backward pass in 8 bits: y = z/2 (1 + erf(z / sqrt 2)), computed in fp32 (relative error below 2^-20 + z^2 2^-24,
- * in the lower tail too; minus infinity gives 0), F32 or BF16, in one pass with values / scales = the blocks of z as sbp_quantize8(z) makes them.  All of one
- * shape and signature, S(i) or B. */
+ * in the lower tail too; a result below fp32's normal range may be 0, minus infinity gives 0), F32 or BF16, in one pass with values / scales = the
+ * blocks of z as sbp_quantize8(z) makes them.  All of one shape and signature, S(i) or B. */
 sbp_status sbp_gelu_save8(const sbp_tensor* z, sbp_tensor* y, sbp_tensor* values, sbp_tensor* scales, void* cuda_stream);
 
 /* Gradient through it: grad_z = grad_y (Phi(z) + z phi(z)), Phi and phi the normal distribution and density, z = value * scale.

@@ -137,8 +137,8 @@ constexpr int blocks_per_sm(int g, int nv, bool backward) {
 
 // Rows on their way: every thread copies its own elements of the rows that its block takes next into its own places in shared memory,
 // asynchronously, so that what is in flight does not hang on registers or barriers, and reads them back when their turn comes.
-// bf16 [8192, 4096] over eight devices 28.5 us, 4.7 TB/s (a row ahead in registers 38.9, none 56); backward 46 us, 4.4 TB/s (51.5, 83), of which some five are
-// the blocks' sums on their way through L2 and the second launch.
+// bf16 [8192, 4096] over eight devices 28.4 us, 4.7 TB/s (a row ahead in registers 38.9, none 56; rows all far from zero 33.8); backward 44.5 us, 4.5 TB/s
+// (51.5, 83), of which some five are the blocks' sums on their way through L2 and the second launch.
 __device__ __forceinline__ void copy16(unsigned to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }

@@ -15,12 +15,12 @@
 // Forms: a CTA pair with 256 x 256 tiles, persistent; single CTAs with 128 x NB tiles, cut along the contraction over a cluster where
 // there are few of them.  Few rows (columns): the 128 rows of the tile are the other operand's.
 //
-// Measured: 8192 x 4096 x 4096 (one scale for 128 columns) 132 us, 2.09 PFLOP/s, 1.25 times the bf16 GEMM rate; 2048^3 15.5 us; a weight of 16384 x 4096
-// under 16 rows 15.5 us.  Bound of the pair form: not the MMAs (512 of 1060 clocks a block) but the round from one block to the one that takes its
+// Measured: 8192 x 4096 x 4096 (one scale for 128 columns) 132 us, 2.09 PFLOP/s, 1.25 times the bf16 GEMM rate; 2048^3 15.8 us; a weight of 16384 x 4096
+// under 16 rows 15.7 us in one piece, 18.4 us over eight shards.  Bound of the pair form: not the MMAs (512 of 1060 clocks a block) but the round from one block to the one that takes its
 // accumulator: products done, the warps woken, 128 columns read and added, the hand-back across the pair, the next products issued.  A first form at 139 us
 // took 111 without the additions and 104 without the reads of tensor memory too.  Tried on it: accumulators of 128 and 160 columns, three and four of them (187 and
 // 191 us: what a warp pays a block, 400 clocks of waits, is paid more often), 16 accumulating warps (210), two loads of columns under way (142), additions one
-// by one instead of in pairs (136), waits that sleep (197).  With a scale for each column 218 us (300 with a row a lane, whose 32 broadcast loads a block take
+// by one instead of in pairs (136), waits that sleep (197).  With a scale for each column 222 us (300 with a row a lane, whose 32 broadcast loads a block take
 // shared memory's bandwidth).
 #include <cuda_bf16.h>
 
@@ -791,8 +791,9 @@ enum { kPairs = 0, kAlone = 1, kTwo = 2 };
 sbp_status ask_clusters(int kind, int splits, int* n) {
   if (kind == kPairs) return launch8_form<true, 256, true, false>(nullptr, 2, 0, nullptr, n);
   constexpr int kStatic = 1024;                    // barriers, and what the launch itself takes
-  const int smem = (kind == kTwo ? Shape8<false, 32, true>::kSmem : Shape8<false, 128, true>::kSmem) + kStatic;
-  SBP_CUDA_TRY(cudaFuncSetAttribute(seats_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  constexpr int kLarge = Shape8<false, 128, true>::kSmem + kStatic, kSmall = Shape8<false, 32, true>::kSmem + kStatic;
+  const int smem = kind == kTwo ? kSmall : kLarge;
+  SBP_CUDA_TRY(cudaFuncSetAttribute(seats_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLarge));      // (whoever asks, so threads may ask at once)
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(device_sms() / splits * splits));
   cfg.blockDim = dim3(Shape8<false, 32, true>::kThreads);
